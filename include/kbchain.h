@@ -91,6 +91,56 @@ kbc_status kbc_softmax_xent_scratch(int64_t n, int32_t b, const float *z, const 
                                     double *col_loss, double *loss, float *dz, void *scratch,
                                     size_t bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Embedding lookup with scaling
+ * ------------------------------------------------------------------------
+ *
+ * The words of a question become the vector that its relation logits are taken
+ * from: rows of a table, scaled, one output row per token or pooled per question.
+ * Rows are row-major here, [rows][dim], the transpose of the arrays above:
+ *   ids    : `tokens` ids, id_bytes 4 (int32) or 8 (int64) each.  An id outside
+ *            [0, rows) stands for padding: a row of zeros, no term of a sum, no
+ *            gradient.
+ *   table  : [rows][dim] of `type`, row r at r * stride elements (stride >= dim).
+ *   out, dout, dtable : contiguous, of `type`.
+ * Any element alignment will do.  1 <= rows < 2^31 - 1, tokens <= 2^30, bags <
+ * 2^31 - 1, 1 <= dim <= 65536, else KBC_EINVAL.  Sums are taken in double, in a
+ * fixed order; an output is rounded to float, and to a 16-bit type from there.
+ */
+typedef enum { KBC_F32 = 0, KBC_BF16 = 1, KBC_F16 = 2 } kbc_type;
+
+/* out[t] = scale * table[ids[t]], [tokens][dim]. */
+kbc_status kbc_embed(int64_t tokens, const void *ids, int32_t id_bytes, int64_t rows, int32_t dim,
+                     const void *table, int64_t stride, kbc_type type, float scale, void *out,
+                     void *stream);
+
+/* out[g] = scale * sum over the tokens t of bag g of table[ids[t]], [bags][dim];
+ * mean != 0: divided by the number of those that are no padding.  A bag without
+ * any is zeros.
+ *   offsets : bags + 1 of them, of the ids' integer type, not decreasing: bag g is
+ *             tokens [offsets[g], offsets[g + 1]) (values outside [0, tokens] are
+ *             taken as the nearer end).  NULL: every bag has tokens / bags tokens,
+ *             which has to be whole.
+ *   scratch : kbc_embed_pool_scratch_size bytes (ragged: offsets are given), 16-byte
+ *             aligned, used by this call alone until it has run. */
+size_t kbc_embed_pool_scratch_size(int64_t tokens, int64_t bags, int32_t ragged, int32_t dim,
+                                   kbc_type type, int32_t mean);
+kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int64_t bags,
+                          const void *offsets, int64_t rows, int32_t dim, const void *table,
+                          int64_t stride, kbc_type type, float scale, int32_t mean, void *out,
+                          void *scratch, size_t bytes, void *stream);
+
+/* Gradient of either with respect to the table, fully written, [rows][dim]:
+ *   dtable[v] = sum over t with ids[t] == v of scale * dout[t]          (bags == 0)
+ *               ... of scale (/ tokens of the bag) * dout[bag of t]     (bags > 0)
+ * Rows that no token names are zeros. */
+size_t kbc_embed_backward_scratch_size(int64_t tokens, int64_t bags, int32_t dim, kbc_type type,
+                                       int32_t mean);
+kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes, int64_t bags,
+                              const void *offsets, int64_t rows, int32_t dim, const void *dout,
+                              kbc_type type, float scale, int32_t mean, void *dtable,
+                              void *scratch, size_t bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

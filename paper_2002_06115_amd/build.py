@@ -115,13 +115,16 @@ def fingerprint(defines, path, bdir, csrc=CSRC) -> dict:
 CHAIN_LIB = os.path.join(OUT_DIR, "libkbchain.so")
 
 
+CHAIN_SOURCES = ["chain_glue.hip", "embed.hip"]
+
+
 def build_chain(verbose: bool = False) -> str:
     """Compile the multi-hop chain glue (include/kbchain.h) into its own
     shared library."""
     os.makedirs(OUT_DIR, exist_ok=True)
     tmp = CHAIN_LIB + ".tmp"
     cmd = [hipcc(), "-x", "hip", *DEVICE_FLAGS, *COMMON_FLAGS, "-shared",
-           os.path.join(CSRC, "chain_glue.hip"), "-o", tmp]
+           *[os.path.join(CSRC, f) for f in CHAIN_SOURCES], "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)

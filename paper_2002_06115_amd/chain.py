@@ -6,6 +6,10 @@ entity weights, and the softmax cross-entropy of the last hop -- each with its
 backward.  Every array is a contiguous float32 [n][b] CUDA tensor (one column
 per example), as for the follow operation; reductions run in double on the
 GPU.  Argument marshalling only: every step runs in the library's kernels.
+
+Before the hops stand the question's words: embed() looks up rows of a table,
+scaled, one a token or pooled per question.  It is differentiable; its gradient
+is embed_backward().
 """
 from __future__ import annotations
 
@@ -39,7 +43,18 @@ _softmax_backward.argtypes = [_I64, _I32, _P, _P, _P, _P, _SZ, _P]
 _l1_normalize.argtypes = [_I64, _I32, _P, _P, _P, _P, _SZ, _P]
 _l1_normalize_backward.argtypes = [_I64, _I32, _P, _P, _P, _P, _P, _SZ, _P]
 _softmax_xent.argtypes = [_I64, _I32, _P, _P, _P, _P, _P, _P, _SZ, _P]
-for _f in (_softmax, _softmax_backward, _l1_normalize, _l1_normalize_backward, _softmax_xent):
+_F32 = ctypes.c_float
+_lib.kbc_embed.argtypes = [_I64, _P, _I32, _I64, _I32, _P, _I64, _I32, _F32, _P, _P]
+_lib.kbc_embed_pool_scratch_size.argtypes = [_I64, _I64, _I32, _I32, _I32, _I32]
+_lib.kbc_embed_pool_scratch_size.restype = _SZ
+_lib.kbc_embed_pool.argtypes = [_I64, _P, _I32, _I64, _P, _I64, _I32, _P, _I64, _I32, _F32, _I32,
+                                _P, _P, _SZ, _P]
+_lib.kbc_embed_backward_scratch_size.argtypes = [_I64, _I64, _I32, _I32, _I32]
+_lib.kbc_embed_backward_scratch_size.restype = _SZ
+_lib.kbc_embed_backward.argtypes = [_I64, _P, _I32, _I64, _P, _I64, _I32, _P, _I32, _F32, _I32,
+                                    _P, _P, _SZ, _P]
+for _f in (_softmax, _softmax_backward, _l1_normalize, _l1_normalize_backward, _softmax_xent,
+           _lib.kbc_embed, _lib.kbc_embed_pool, _lib.kbc_embed_backward):
     _f.restype = ctypes.c_int
 
 
@@ -140,3 +155,166 @@ def softmax_xent(z, t):
                       loss.data_ptr(), dz.data_ptr(), scratch, size, _stream(z)),
         "kbc_softmax_xent")
     return loss, col, dz
+
+
+# -- embedding lookup ----------------------------------------------------------
+
+_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+
+
+def _type(t, name):
+    """The library's code of a CUDA tensor's type."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or str(t.dtype) not in _TYPES:
+        raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA tensor")
+    return _TYPES[str(t.dtype)]
+
+
+def _ints(t, name, device, dims, dtype=None):
+    """A contiguous int32 or int64 tensor on `device`, of one of `dims` dimensions."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or \
+            t.device != device:
+        raise TypeError(f"{name} must be an int32 or int64 tensor on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, as the ids are")
+    if t.dim() not in dims or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of {' or '.join(map(str, dims))} dimensions")
+    return t
+
+
+def _run(fn, what, device, *args):
+    """fn(*args, stream) on the current stream of `device`, with that device current."""
+    import torch
+    stream = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, stream)
+    _ok(status, what)
+
+
+def _bytes(n, device):
+    """(tensor, address, bytes) of n bytes of scratch; the tensor is held until
+    the call is enqueued."""
+    import torch
+    if n == 0:
+        return None, None, 0
+    s = torch.empty(n, dtype=torch.uint8, device=device)
+    return s, s.data_ptr(), n
+
+
+def _bag_args(ids, offsets, pool, device):
+    """(bags, offsets' address) of a lookup: bags is None where there is no pooling."""
+    if pool not in (None, "sum", "mean"):
+        raise ValueError('pool must be None, "sum" or "mean"')
+    if pool is None:
+        if offsets is not None:
+            raise ValueError('offsets go with pool="sum" or "mean"')
+        _ints(ids, "ids", device, range(1, 9))
+        return None, None
+    if offsets is None:
+        return _ints(ids, "ids", device, (2,)).shape[0], None
+    _ints(ids, "ids", device, (1,))
+    _ints(offsets, "offsets", device, (1,), ids.dtype)
+    if offsets.numel() < 1:
+        raise ValueError("offsets must hold one value more than there are bags")
+    return offsets.numel() - 1, offsets.data_ptr()
+
+
+def _embed_forward(table, ids, offsets, scale, pool):
+    import torch
+    code = _type(table, "table")
+    if table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 1:
+        raise ValueError("table must be [rows][dim], not empty")
+    rows, dim = table.shape
+    if (dim > 1 and table.stride(1) != 1) or (rows > 1 and table.stride(0) < dim):
+        raise ValueError("the values of a row of table must be adjacent, its rows apart")
+    stride = max(table.stride(0), dim)
+    device = table.device
+    bags, at = _bag_args(ids, offsets, pool, device)
+    width, n = ids.element_size(), ids.numel()
+    if bags is None:
+        out = torch.empty((*ids.shape, dim), dtype=table.dtype, device=device)
+        _run(_lib.kbc_embed, "kbc_embed", device, n, ids.data_ptr(), width, rows, dim,
+             table.data_ptr(), stride, code, float(scale), out.data_ptr())
+        return out
+    out = torch.empty((bags, dim), dtype=table.dtype, device=device)
+    mean = int(pool == "mean")
+    held, scratch, size = _bytes(_lib.kbc_embed_pool_scratch_size(
+        n, bags, offsets is not None, dim, code, mean), device)
+    _run(_lib.kbc_embed_pool, "kbc_embed_pool", device, n, ids.data_ptr(), width, bags, at, rows,
+         dim, table.data_ptr(), stride, code, float(scale), mean, out.data_ptr(), scratch, size)
+    return out
+
+
+def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
+    """The gradient [rows][dim] of embed's table, of dout's type, for the upstream
+    gradient dout of its output; rows that no id names are zeros."""
+    import torch
+    code = _type(dout, "dout")
+    device = dout.device
+    bags, at = _bag_args(ids, offsets, pool, device)
+    lead = tuple(ids.shape) if bags is None else (bags,)
+    if dout.dim() != len(lead) + 1 or tuple(dout.shape[:-1]) != lead or dout.shape[-1] < 1 or \
+            not dout.is_contiguous():
+        raise ValueError(f"dout must be contiguous, of shape {lead} and a row's width")
+    dim, n, mean = dout.shape[-1], ids.numel(), int(pool == "mean")
+    if bags == 0:
+        n = 0  # tokens of no bag
+    dtable = torch.empty((rows, dim), dtype=dout.dtype, device=device)
+    held, scratch, size = _bytes(_lib.kbc_embed_backward_scratch_size(
+        n, bags or 0, dim, code, mean), device)
+    _run(_lib.kbc_embed_backward, "kbc_embed_backward", device, n, ids.data_ptr(),
+         ids.element_size(), bags or 0, at, rows, dim, dout.data_ptr(), code, float(scale), mean,
+         dtable.data_ptr(), scratch, size)
+    return dtable
+
+
+_functions = {}
+
+
+def _function(name):
+    """The autograd function of an operation of this module (torch is imported
+    where it is needed)."""
+    if name not in _functions:
+        _functions.update(_make_functions())
+    return _functions[name]
+
+
+def _make_functions():
+    import torch
+
+    class Embed(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, table, ids, offsets, scale, pool):
+            ctx.save_for_backward(ids, offsets)
+            ctx.args = table.shape[0], table.dtype, scale, pool
+            return _embed_forward(table, ids, offsets, scale, pool)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dout):
+            ids, offsets = ctx.saved_tensors
+            rows, dtype, scale, pool = ctx.args
+            return (embed_backward(dout.to(dtype).contiguous(), ids, rows, offsets, scale, pool),
+                    None, None, None, None)
+
+    return {"embed": Embed}
+
+
+def embed(table, ids, offsets=None, scale=1.0, pool=None):
+    """Rows of table [rows][dim] (float32, bfloat16 or float16), times scale.
+
+    Without pooling, ids.shape + (dim,): one row an id.  With pool="sum" or "mean",
+    [bags][dim]: the sum, or the mean, over each bag's ids, which are the rows of a
+    2-D ids, or with offsets (bags + 1 of them, not decreasing, of the ids' type)
+    ids[offsets[g]:offsets[g + 1]] of a 1-D ids.  An id outside [0, rows) stands for
+    padding: zeros, no term, not counted by the mean, no gradient; a bag of nothing
+    else is zeros.  Differentiable with respect to table.
+    """
+    import torch
+    if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
+        return _function("embed").apply(table, ids, offsets, scale, pool)
+    return _embed_forward(table, ids, offsets, scale, pool)

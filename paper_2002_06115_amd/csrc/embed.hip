@@ -1,0 +1,885 @@
+// embed.hip -- embedding lookup with scaling, plain and pooled, and its gradient
+// by sorted tokens (kbchain.h: kbc_embed, kbc_embed_pool, kbc_embed_backward).
+//
+//     out[t] = scale * table[ids[t]]                                (plain)
+//     out[g] = scale (/ tokens of g) * sum over t in g of table[ids[t]]   (pooled)
+//     dtable[v] = sum over t with ids[t] == v of scale (/ tokens of g(t)) *
+//                 dout[t or g(t)]
+//
+// All of it moves rows: a lane group of LPG lanes reads a row of dim values 16
+// bytes a lane (a row whose width is not a multiple of that ends in a lane that
+// takes its last 16 bytes again), several rows in flight.  A pooled sum over few
+// tokens is one workgroup a bag.  The gradient, and pooled sums over many
+// tokens, are one segmented sum: a list of (row of the output, row read), sorted
+// by the first, is cut into equal chunks, one a lane group, that are walked in
+// order; a row that lies inside its chunk is written at once, a row that crosses
+// chunks leaves one partial sum per chunk, added in order by the second launch.
+// So the work is spread evenly however often a word occurs, nothing is atomic,
+// and two calls give the same bits.  Sums are taken in double; an output is
+// rounded to float and, in a 16-bit type, from there to the type.
+//
+// The list is sorted by the tokens' ids, stably.  Up to kRankTokens tokens, each
+// token's place is counted: the number of tokens with a smaller id, or the same
+// and before it, against all ids in LDS, in one launch over the whole chip.
+// More take a radix sort, up to 9 bits a pass, three launches each.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "kbchain.h"
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWave = 64;
+
+// -- rows of a type ---------------------------------------------------------------
+
+// 16 bytes of a row, wherever the row begins.
+template <class T>
+struct Row {
+  static constexpr int kVec = 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+template <class T, int VEC>
+__device__ __forceinline__ void load_vals(const T *p, T (&v)[VEC]) {
+  if constexpr (VEC == 1) {
+    v[0] = *p;
+  } else {
+    const typename Row<T>::vec t = *reinterpret_cast<const typename Row<T>::vec *>(p);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v[k] = t[k];
+  }
+}
+
+// Output rows are written once and not read again by these kernels.
+template <class T, int VEC>
+__device__ __forceinline__ void store_vals(T *p, const T (&v)[VEC]) {
+  if constexpr (VEC == 1) {
+    *p = v[0];
+  } else {
+    typename Row<T>::vec t;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) t[k] = v[k];
+    __builtin_nontemporal_store(t, reinterpret_cast<typename Row<T>::vec *>(p));
+  }
+}
+
+// The ids and offsets of a call, int32 or int64.
+struct Ints {
+  const void *p;
+  int bytes;
+};
+__device__ __forceinline__ int64_t load_int(const Ints &a, int64_t i) {
+  return a.bytes == 8 ? static_cast<const int64_t *>(a.p)[i]
+                      : (int64_t)static_cast<const int32_t *>(a.p)[i];
+}
+
+// How tokens are grouped into bags: bag g holds tokens [begin(g), begin(g + 1)).
+struct Bags {
+  int64_t n;       // 0: every token is an output row of its own
+  Ints offsets;    // null: n bags of `each` tokens
+  int64_t each;
+  int64_t tokens;
+};
+__device__ __forceinline__ int64_t bag_begin(const Bags &b, int64_t g) {
+  if (!b.offsets.p) return g * b.each;
+  const int64_t o = load_int(b.offsets, g);
+  return o < 0 ? 0 : o > b.tokens ? b.tokens : o;  // never a token past the last
+}
+// The bag of token t, -1 where it is in none.
+__device__ __forceinline__ int64_t bag_of(const Bags &b, int64_t t) {
+  if (!b.offsets.p) return t / b.each;
+  int64_t lo = 0, hi = b.n + 1;  // offsets [0, lo) are <= t, [hi, n] are > t
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (bag_begin(b, mid) <= t)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  return lo >= 1 && lo <= b.n ? lo - 1 : -1;
+}
+
+// -- plain lookup -------------------------------------------------------------------
+
+struct LookupArgs {
+  Ints ids;
+  int64_t tokens, rows;
+  int32_t dim;
+  const void *table;
+  int64_t stride;
+  float scale;
+  void *out;
+};
+
+// Rows of one lane group in flight.
+constexpr int kLookupRows = 4;
+
+template <class T, int VEC, int LPG>
+__global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a) {
+  constexpr int GPB = kThreads / LPG;
+  const int lane = threadIdx.x % LPG;
+  const int64_t t0 = ((int64_t)blockIdx.x * GPB + threadIdx.x / LPG) * kLookupRows;
+  const T *table = static_cast<const T *>(a.table);
+  T *out = static_cast<T *>(a.out);
+  int64_t id[kLookupRows];
+#pragma unroll
+  for (int k = 0; k < kLookupRows; ++k) {
+    id[k] = t0 + k < a.tokens ? load_int(a.ids, t0 + k) : -1;
+    if (id[k] >= a.rows) id[k] = -1;
+  }
+  for (int c0 = lane * VEC; c0 < a.dim; c0 += LPG * VEC) {
+    const int c = min(c0, a.dim - VEC);
+    T v[kLookupRows][VEC];
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k)
+      if (id[k] >= 0) load_vals<T, VEC>(table + id[k] * a.stride + c, v[k]);
+#pragma unroll
+    for (int k = 0; k < kLookupRows; ++k) {
+      if (t0 + k >= a.tokens) break;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[k][i] = id[k] >= 0 ? (T)((float)v[k][i] * a.scale) : (T)0.0f;
+      store_vals<T, VEC>(out + (t0 + k) * a.dim + c, v[k]);
+    }
+  }
+}
+
+// -- pooled lookup, a workgroup per bag ---------------------------------------------
+
+struct PoolArgs {
+  Ints ids;
+  Bags bags;
+  int64_t rows;
+  int32_t dim, mean;
+  const void *table;
+  int64_t stride;
+  float scale;
+  void *out;
+};
+
+constexpr int kPoolRows = 4;
+
+template <class T, int VEC, int LPG>
+__global__ __launch_bounds__(kThreads) void pool_kernel(PoolArgs a) {
+  constexpr int GPB = kThreads / LPG;
+  __shared__ double part[GPB][LPG * VEC];
+  __shared__ int counts[GPB];
+  const int lane = threadIdx.x % LPG, grp = threadIdx.x / LPG;
+  const int64_t g = blockIdx.x;
+  const int c0 = blockIdx.y * (LPG * VEC) + lane * VEC;
+  const bool active = c0 < a.dim;
+  const int c = active ? min(c0, a.dim - VEC) : 0;
+  const int64_t begin = bag_begin(a.bags, g), end = bag_begin(a.bags, g + 1);
+  const T *table = static_cast<const T *>(a.table);
+  double acc[VEC];
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+  for (int64_t t0 = begin + grp; t0 < end; t0 += GPB * kPoolRows) {
+    int64_t id[kPoolRows];
+    T v[kPoolRows][VEC];
+#pragma unroll
+    for (int k = 0; k < kPoolRows; ++k) {
+      id[k] = t0 + k * GPB < end ? load_int(a.ids, t0 + k * GPB) : -1;
+      if (id[k] >= a.rows) id[k] = -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kPoolRows; ++k)
+      if (id[k] >= 0) load_vals<T, VEC>(table + id[k] * a.stride + c, v[k]);
+#pragma unroll
+    for (int k = 0; k < kPoolRows; ++k)
+      if (id[k] >= 0) {
+        ++count;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += (double)(float)v[k][i];
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) part[grp][lane * VEC + i] = acc[i];
+  if (lane == 0) counts[grp] = count;
+  __syncthreads();
+  if (grp != 0 || !active) return;
+  for (int k = 1; k < GPB; ++k) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] += part[k][lane * VEC + i];
+    count += counts[k];
+  }
+  const double w = (double)a.scale / (a.mean && count > 0 ? (double)count : 1.0);
+  T y[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) y[i] = (T)(float)(acc[i] * w);
+  store_vals<T, VEC>(static_cast<T *>(a.out) + g * a.dim + c, y);
+}
+
+// -- the list of a segmented sum ------------------------------------------------------
+//
+// Entries (row of the output, row read): for the gradient (id, token or bag),
+// for a pooled sum (bag, id).  An entry whose second field is -1 adds nothing, one
+// whose first is the number of output rows is of no row.
+
+struct ListArgs {
+  Ints ids;
+  Bags bags;
+  int64_t tokens, rows;
+  int32_t mean;
+  double *weights;  // with mean: 1 / tokens of each bag (0: none)
+  void *fill;       // output rows to clear, in words of 4 bytes and a rest of 2
+  int64_t fill_bytes;
+  int2 *entries;
+  // workgroups of the launch: list_wgs make the list, then weight_wgs, then the fill's
+  uint32_t list_wgs, weight_wgs;
+};
+
+// Token t's key in the gradient's list: its id, or `rows` where it names none.
+__device__ __forceinline__ int key_of(const ListArgs &a, int64_t t) {
+  const int64_t id = load_int(a.ids, t);
+  return id < 0 || id >= a.rows ? (int)a.rows : (int)id;
+}
+__device__ __forceinline__ int2 grad_entry(const ListArgs &a, int key, int64_t t) {
+  const int64_t src = a.bags.n ? bag_of(a.bags, t) : t;
+  return make_int2(key, (int)src);
+}
+
+// 1 / tokens of four bags, a wave each; a long one by the whole workgroup.
+constexpr int64_t kLongBag = 4096;
+__device__ __forceinline__ int count_ids(const ListArgs &a, int64_t begin, int64_t end, int lane,
+                                         int lanes) {
+  int n = 0;
+  for (int64_t t = begin + lane; t < end; t += lanes) {
+    const int64_t id = load_int(a.ids, t);
+    n += id >= 0 && id < a.rows;
+  }
+  for (int m = 1; m < kWave; m <<= 1) n += __shfl_xor(n, m);
+  return n;
+}
+__device__ void bag_weights(const ListArgs &a, int64_t block) {
+  __shared__ int counts[kThreads / kWave];
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  for (int k = 0; k < kThreads / kWave; ++k) {
+    const int64_t g = block * (kThreads / kWave) + k;
+    if (g >= a.bags.n) break;
+    const int64_t begin = bag_begin(a.bags, g), end = bag_begin(a.bags, g + 1);
+    if (end - begin < kLongBag) {  // the same for the whole workgroup
+      if (k != wave) continue;
+      const int n = count_ids(a, begin, end, lane, kWave);
+      if (lane == 0) a.weights[g] = n > 0 ? 1.0 / (double)n : 0.0;
+    } else {
+      const int n = count_ids(a, begin, end, threadIdx.x, kThreads);
+      __syncthreads();
+      if (lane == 0) counts[wave] = n;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        int all = 0;
+        for (int w = 0; w < kThreads / kWave; ++w) all += counts[w];
+        a.weights[g] = all > 0 ? 1.0 / (double)all : 0.0;
+      }
+    }
+  }
+}
+
+// 64 KB of zeros from each workgroup.
+typedef unsigned int fill_vec __attribute__((ext_vector_type(4), aligned(2)));
+constexpr int64_t kFillBytes = 16 * kThreads * 16;
+__device__ __forceinline__ void clear(const ListArgs &a, int64_t block) {
+  char *p = static_cast<char *>(a.fill);
+  const int64_t end = min(a.fill_bytes, (block + 1) * kFillBytes);
+  for (int64_t i = block * kFillBytes + (int64_t)threadIdx.x * 16; i < end; i += kThreads * 16) {
+    if (i + 16 <= end) {
+      const fill_vec zero = {0, 0, 0, 0};
+      __builtin_nontemporal_store(zero, reinterpret_cast<fill_vec *>(p + i));
+    } else {
+      for (int64_t j = i; j < end; j += 2) *reinterpret_cast<uint16_t *>(p + j) = 0;
+    }
+  }
+}
+
+// What the workgroups past list_wgs of a list's first launch do.
+__device__ __forceinline__ bool other_work(const ListArgs &a) {
+  if (blockIdx.x < a.list_wgs) return false;
+  const uint32_t k = blockIdx.x - a.list_wgs;
+  if (k < a.weight_wgs)
+    bag_weights(a, k);
+  else
+    clear(a, k - a.weight_wgs);
+  return true;
+}
+
+// A pooled sum's list, which is in order as it is.
+__global__ __launch_bounds__(kThreads) void pool_list_kernel(ListArgs a) {
+  if (other_work(a)) return;
+  const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (t >= a.tokens) return;
+  const int64_t g = bag_of(a.bags, t), id = load_int(a.ids, t);
+  // A token before the first bag or behind the last one is of no row: bags.n.
+  a.entries[t] = make_int2(g < 0 ? (int)a.bags.n : (int)g,
+                           id < 0 || id >= a.rows ? -1 : (int)id);
+}
+
+// -- the gradient's list, few tokens: places counted ----------------------------------
+
+constexpr int64_t kRankTokens = 8192;
+constexpr int kRankLanes = 8;                          // lanes that share a token's count
+constexpr int kRankPer = kThreads / kRankLanes;        // tokens of a workgroup
+
+__global__ __launch_bounds__(kThreads) void rank_kernel(ListArgs a) {
+  if (other_work(a)) return;
+  extern __shared__ int4 rank_lds[];
+  int *keys = reinterpret_cast<int *>(rank_lds);
+  const int n = (int)a.tokens, quads = (n + 3) / 4;
+  for (int t = threadIdx.x; t < quads * 4; t += kThreads)
+    keys[t] = t < n ? key_of(a, t) : INT32_MAX;
+  __syncthreads();
+  const int lane = threadIdx.x % kRankLanes;
+  const int t = blockIdx.x * kRankPer + threadIdx.x / kRankLanes;
+  const int key = keys[min(t, n - 1)];
+  // Four keys at a time; those of t's own four are told apart one by one.
+  int place = 0;
+  const int own = t / 4;
+  for (int q = lane; q < quads; q += kRankLanes) {
+    const int4 k = rank_lds[q];
+    const int bar = q < own ? key : key - 1;  // (keys are not negative)
+    place += (k.x <= bar) + (k.y <= bar) + (k.z <= bar) + (k.w <= bar);
+  }
+  if (lane == own % kRankLanes)
+    for (int j = own * 4; j < t && j < n; ++j) place += keys[j] == key;
+#pragma unroll
+  for (int m = 1; m < kRankLanes; m <<= 1) place += __shfl_xor(place, m);
+  if (lane == 0 && t < n) a.entries[place] = grad_entry(a, key, t);
+}
+
+// -- the gradient's list, many tokens: radix sort -------------------------------------
+
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kTileItems = 8, kTile = kThreads * kTileItems;
+
+struct RadixArgs {
+  ListArgs list;
+  const int2 *in;    // null: the tokens themselves
+  int2 *out;
+  int32_t shift, bits;
+  uint32_t tiles;
+  uint32_t *counts;  // [digit][tile]; after the scan, entries of the digit in the tiles before
+  uint32_t *totals;  // [digit]
+};
+
+__device__ __forceinline__ int radix_key(const RadixArgs &a, int64_t i) {
+  return a.in ? a.in[i].x : key_of(a.list, i);
+}
+
+__global__ __launch_bounds__(kThreads) void radix_count_kernel(RadixArgs a) {
+  if (other_work(a.list)) return;
+  __shared__ uint32_t count[kDigits];
+  const int digits = 1 << a.bits;
+  for (int i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
+  __syncthreads();
+  const int64_t base = (int64_t)blockIdx.x * kTile;
+#pragma unroll
+  for (int k = 0; k < kTileItems; ++k) {
+    const int64_t i = base + k * kThreads + threadIdx.x;
+    if (i < a.list.tokens) atomicAdd(&count[(radix_key(a, i) >> a.shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < digits; i += kThreads)
+    a.counts[(int64_t)i * a.tiles + blockIdx.x] = count[i];
+}
+
+// The sum of v over the threads before this one, and over all of them.
+__device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *lds, uint32_t *all) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  uint32_t x = v;
+#pragma unroll
+  for (int m = 1; m < kWave; m <<= 1) {
+    const uint32_t y = __shfl_up(x, m);
+    if (lane >= m) x += y;
+  }
+  __syncthreads();  // earlier readers of lds are done
+  if (lane == kWave - 1) lds[wave] = x;
+  __syncthreads();
+  uint32_t before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) {
+    if (w < wave) before += lds[w];
+    sum += lds[w];
+  }
+  *all = sum;
+  return before + x - v;
+}
+
+// One workgroup per digit: its counts become the entries in the tiles before.
+__global__ __launch_bounds__(kThreads) void radix_scan_kernel(uint32_t tiles, uint32_t *counts,
+                                                              uint32_t *totals) {
+  __shared__ uint32_t lds[kThreads / kWave];
+  uint32_t *c = counts + (int64_t)blockIdx.x * tiles;
+  uint32_t sum = 0;
+  for (uint32_t i0 = 0; i0 < tiles; i0 += kThreads) {
+    const uint32_t i = i0 + threadIdx.x;
+    const uint32_t v = i < tiles ? c[i] : 0;
+    uint32_t all;
+    const uint32_t before = scan_threads(v, lds, &all);
+    if (i < tiles) c[i] = sum + before;
+    sum += all;
+  }
+  if (threadIdx.x == 0) totals[blockIdx.x] = sum;
+}
+
+// Each wave places 512 consecutive entries, 64 at a time in order: lanes of one
+// digit find each other by ballots, and the wave's own counter of the digit
+// gives the place of the first of them.
+__global__ __launch_bounds__(kThreads) void radix_place_kernel(RadixArgs a) {
+  constexpr int kWaves = kThreads / kWave;
+  // Lanes of a wave read what others of it wrote: volatile keeps every access.
+  __shared__ volatile uint32_t count[kWaves][kDigits];
+  __shared__ uint32_t base[kDigits];
+  __shared__ uint32_t lds[kWaves];
+  const int digits = 1 << a.bits;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) count[i / kDigits][i % kDigits] = 0;
+  {  // where each digit's entries begin
+    constexpr int kPer = kDigits / kThreads;
+    uint32_t v[kPer], sum = 0, all;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = threadIdx.x * kPer + k;
+      v[k] = i < digits ? a.totals[i] : 0;
+      sum += v[k];
+    }
+    uint32_t at = scan_threads(sum, lds, &all);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = threadIdx.x * kPer + k;
+      base[i] = at + (i < digits ? a.counts[(int64_t)i * a.tiles + blockIdx.x] : 0);
+      at += v[k];
+    }
+  }
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTileItems * kWave);
+  int2 e[kTileItems];
+  int digit[kTileItems];
+  uint32_t place[kTileItems];
+#pragma unroll
+  for (int k = 0; k < kTileItems; ++k) {
+    const int64_t i = first + k * kWave + lane;
+    digit[k] = -1;
+    if (i < a.list.tokens) {
+      e[k] = a.in ? a.in[i] : grad_entry(a.list, key_of(a.list, i), i);
+      digit[k] = (e[k].x >> a.shift) & (digits - 1);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kTileItems; ++k) {
+    const bool valid = digit[k] >= 0;
+    unsigned long long same = __ballot(valid);
+    for (int bit = 0; bit < a.bits; ++bit) {
+      const bool set = valid && (digit[k] >> bit & 1);
+      const unsigned long long m = __ballot(set);
+      same &= set ? m : ~m;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    const uint32_t before = valid ? count[wave][digit[k]] : 0;
+    place[k] = before + rank;
+    __builtin_amdgcn_wave_barrier();
+    if (valid && rank == 0) count[wave][digit[k]] = before + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kTileItems; ++k)
+    if (digit[k] >= 0) {
+      uint32_t at = base[digit[k]] + place[k];
+      for (int w = 0; w < wave; ++w) at += count[w][digit[k]];
+      a.out[at] = e[k];
+    }
+}
+
+// -- the segmented sum ------------------------------------------------------------------
+
+struct SumArgs {
+  const int2 *entries;
+  int64_t n;
+  int32_t chunk;
+  const void *src;
+  int64_t src_stride;
+  int32_t dim;
+  const double *src_weights;  // of the rows read, or null
+  const double *out_weights;  // of the rows written, or null
+  double scale;
+  void *out;
+  int64_t out_rows;
+  double *slots;  // [chunk][2][dim]: the sum of the chunk's first row, if it began before
+                  // the chunk, and of its last one, if that goes on behind it
+};
+
+constexpr int kSumRows = 8;  // of a lane group in flight
+
+template <class T, int VEC>
+__device__ __forceinline__ void write_row(const SumArgs &a, int key, int c,
+                                          const double (&acc)[VEC]) {
+  if (key < 0 || key >= a.out_rows) return;
+  const double w = a.out_weights ? a.scale * a.out_weights[key] : a.scale;
+  T y[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) y[i] = (T)(float)(acc[i] * w);
+  store_vals<T, VEC>(static_cast<T *>(a.out) + (int64_t)key * a.dim + c, y);
+}
+
+template <class T, int VEC, int LPG>
+__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
+  constexpr int GPB = kThreads / LPG;
+  const int lane = threadIdx.x % LPG;
+  const int64_t q = (int64_t)blockIdx.x * GPB + threadIdx.x / LPG;
+  const int c0 = blockIdx.y * (LPG * VEC) + lane * VEC;
+  const int64_t p0 = q * a.chunk, p1 = min(a.n, p0 + a.chunk);
+  if (p0 >= a.n || c0 >= a.dim) return;  // no barrier below
+  const int c = min(c0, a.dim - VEC);
+  const T *src = static_cast<const T *>(a.src);
+  int key = a.entries[p0].x;
+  bool began = p0 == 0 || a.entries[p0 - 1].x != key;  // the current row began in this chunk
+  double acc[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+  auto slot = [&](int which) {
+    double *s = a.slots + (q * 2 + which) * a.dim + c;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) s[i] = acc[i];
+  };
+  for (int64_t p = p0; p < p1; p += kSumRows) {
+    int2 e[kSumRows];
+    T v[kSumRows][VEC];
+    double w[kSumRows];
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) e[k] = a.entries[min(p + k, p1 - 1)];
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) {
+      const int r = max(e[k].y, 0);
+      load_vals<T, VEC>(src + (int64_t)r * a.src_stride + c, v[k]);
+      w[k] = a.src_weights ? a.src_weights[r] : 1.0;
+    }
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) {
+      if (p + k >= p1) break;
+      if (e[k].x != key) {
+        if (began)
+          write_row<T, VEC>(a, key, c, acc);
+        else
+          slot(0);
+        began = true;
+        key = e[k].x;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+      }
+      if (e[k].y >= 0) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += (double)(float)v[k][i] * w[k];
+      }
+    }
+  }
+  if (p1 < a.n && a.entries[p1].x == key)
+    slot(began ? 1 : 0);
+  else if (began)
+    write_row<T, VEC>(a, key, c, acc);
+  else
+    slot(0);
+}
+
+// Rows that cross chunks: the workgroup of the chunk where the row began adds its
+// partial sums, the chunks' in order over the lane groups, the groups' in order.
+constexpr int kJoinCols = 64;  // columns of a workgroup
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a) {
+  constexpr int GPB = kThreads / kJoinCols;
+  __shared__ double part[GPB][kJoinCols];
+  const int64_t q = blockIdx.x, p0 = q * a.chunk, p1 = p0 + a.chunk;
+  if (p1 >= a.n) return;
+  const int key = a.entries[p1].x;
+  if (a.entries[p1 - 1].x != key || key >= a.out_rows || key < 0) return;
+  if (p0 > 0 && a.entries[p0 - 1].x == key) return;  // it began before
+  // Chunks q + 1 .. last begin in the row.
+  const int lane = threadIdx.x % kWave;
+  int64_t last = q;
+  for (;;) {
+    const int64_t at = (last + 1 + lane) * a.chunk;
+    const unsigned long long in = __ballot(at < a.n && a.entries[min(at, a.n - 1)].x == key);
+    if (in == ~0ull) {
+      last += kWave;
+    } else {
+      last += __builtin_ctzll(~in);
+      break;
+    }
+  }
+  const int grp = threadIdx.x / kJoinCols, col = threadIdx.x % kJoinCols;
+  const int c = blockIdx.y * kJoinCols + col;
+  const bool active = c < a.dim;
+  double acc = 0.0;
+  if (active)
+    for (int64_t k = q + grp; k <= last; k += GPB)
+      acc += a.slots[(k * 2 + (k == q ? 1 : 0)) * a.dim + c];
+  part[grp][col] = acc;
+  __syncthreads();
+  if (grp != 0 || !active) return;
+  for (int k = 1; k < GPB; ++k) acc += part[k][col];
+  const double sum[1] = {acc};
+  write_row<T, 1>(a, key, c, sum);
+}
+
+// -- how a call is launched ----------------------------------------------------------------
+
+int lanes_for(int32_t dim, int vec) {
+  const int lanes = (dim + vec - 1) / vec;
+  int lpg = 1;
+  while (lpg < lanes && lpg < kWave) lpg <<= 1;
+  return lpg;
+}
+
+// f(T{}, vec, lanes) for the type and width of a call's rows, as constants.
+template <class T, class F>
+void with_lanes(int32_t dim, F f) {
+  constexpr int V = Row<T>::kVec;
+  const bool wide = dim >= V;
+  const int lpg = lanes_for(dim, wide ? V : 1);
+  auto go = [&](auto lanes) {
+    if (wide)
+      f(T{}, std::integral_constant<int, V>{}, lanes);
+    else
+      f(T{}, std::integral_constant<int, 1>{}, lanes);
+  };
+  switch (lpg) {
+    case 1: go(std::integral_constant<int, 1>{}); break;
+    case 2: go(std::integral_constant<int, 2>{}); break;
+    case 4: go(std::integral_constant<int, 4>{}); break;
+    case 8: go(std::integral_constant<int, 8>{}); break;
+    case 16: go(std::integral_constant<int, 16>{}); break;
+    case 32: go(std::integral_constant<int, 32>{}); break;
+    default: go(std::integral_constant<int, 64>{}); break;
+  }
+}
+template <class F>
+void with_rows(kbc_type type, int32_t dim, F f) {
+  switch (type) {
+    case KBC_F32: with_lanes<float>(dim, f); break;
+    case KBC_BF16: with_lanes<__bf16>(dim, f); break;
+    case KBC_F16: with_lanes<_Float16>(dim, f); break;
+  }
+}
+
+int64_t size_of(kbc_type t) { return t == KBC_F32 ? 4 : 2; }
+bool bad_type(kbc_type t) { return t != KBC_F32 && t != KBC_BF16 && t != KBC_F16; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t padded(int64_t bytes) { return (size_t)ceil_div(bytes, 256) * 256; }
+
+kbc_status launched() { return hipGetLastError() == hipSuccess ? KBC_OK : KBC_EHIP; }
+
+// Entries of a chunk: about 4096 waves' worth of lane groups over the list, at
+// least kSumRows entries each.
+int32_t chunk_for(int64_t tokens, int lpg) {
+  int32_t chunk = kSumRows;
+  while (chunk < 128 && tokens * lpg > (int64_t)chunk * 4096 * kWave) chunk *= 2;
+  return chunk;
+}
+
+// Where a call's scratch holds what.
+struct Scratch {
+  size_t entries, sorted, counts, totals, weights, slots, bytes;
+};
+Scratch scratch_for(int64_t tokens, int64_t bags, int32_t dim, bool sorted, bool mean, int lpg) {
+  Scratch s = {};
+  size_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t here = at;
+    at += padded(bytes);
+    return here;
+  };
+  s.entries = take(tokens * 8);
+  if (sorted && tokens > kRankTokens) {
+    s.sorted = take(tokens * 8);
+    s.counts = take((int64_t)kDigits * ceil_div(tokens, kTile) * 4);
+    s.totals = take(kDigits * 4);
+  }
+  if (mean) s.weights = take(bags * 8);
+  const int64_t chunks = ceil_div(tokens, chunk_for(tokens, lpg));
+  if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);
+  s.bytes = at;
+  return s;
+}
+int group_lanes(kbc_type type, int32_t dim) {
+  const int v = type == KBC_F32 ? 4 : 8;
+  return lanes_for(dim, dim >= v ? v : 1);
+}
+
+// A pooled sum takes a workgroup per bag where no bag can be long: few tokens in
+// all, or bags of one, small length.
+constexpr int64_t kMostBlocks = (int64_t(1) << 32) / kThreads - 1;  // a grid's threads fit 32 bits
+bool pools_directly(int64_t tokens, int64_t bags, bool ragged) {
+  return bags <= kMostBlocks && (tokens <= 4096 || (!ragged && tokens / bags <= 512));
+}
+
+void launch_sum(kbc_type type, const SumArgs &a, hipStream_t s) {
+  const int64_t chunks = ceil_div(a.n, a.chunk);
+  with_rows(type, a.dim, [&](auto t, auto vec, auto lanes) {
+    using T = decltype(t);
+    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
+    const dim3 grid((unsigned)ceil_div(chunks, kThreads / L), (unsigned)ceil_div(a.dim, L * V));
+    hipLaunchKernelGGL((sum_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
+  });
+  if (chunks <= 1) return;
+  const dim3 grid((unsigned)chunks, (unsigned)ceil_div(a.dim, kJoinCols));
+  switch (type) {
+    case KBC_F32: hipLaunchKernelGGL(join_kernel<float>, grid, dim3(kThreads), 0, s, a); break;
+    case KBC_BF16: hipLaunchKernelGGL(join_kernel<__bf16>, grid, dim3(kThreads), 0, s, a); break;
+    case KBC_F16: hipLaunchKernelGGL(join_kernel<_Float16>, grid, dim3(kThreads), 0, s, a); break;
+  }
+}
+
+// The grid of a list's first launch, and which of its workgroups do what.
+dim3 list_grid(ListArgs *a, int64_t list_wgs) {
+  a->list_wgs = (uint32_t)list_wgs;
+  a->weight_wgs = a->mean ? (uint32_t)ceil_div(a->bags.n, kThreads / kWave) : 0;
+  return dim3((unsigned)(list_wgs + a->weight_wgs + ceil_div(a->fill_bytes, kFillBytes)));
+}
+
+// A call's sizes: every index into rows, tokens and bags fits an int, and so do
+// the lists' places and grids.
+constexpr int64_t kMostTokens = int64_t(1) << 30;
+constexpr int64_t kMostRows = (int64_t)INT32_MAX - 1;
+bool bad_sizes(int64_t tokens, int64_t bags, int64_t rows, int32_t dim, int32_t id_bytes) {
+  return tokens < 0 || tokens > kMostTokens || bags < 0 || bags > kMostRows || rows < 1 ||
+         rows > kMostRows || dim < 1 || dim > 65536 || (id_bytes != 4 && id_bytes != 8);
+}
+bool bad_scratch(const Scratch &need, const void *scratch, size_t bytes) {
+  return need.bytes > 0 &&
+         (!scratch || bytes < need.bytes || reinterpret_cast<uintptr_t>(scratch) % 16 != 0);
+}
+Bags bags_of(int64_t bags, const void *offsets, int32_t id_bytes, int64_t tokens) {
+  return {bags, {offsets, id_bytes}, bags > 0 ? tokens / bags : 1, tokens};
+}
+
+}  // namespace
+
+extern "C" {
+
+kbc_status kbc_embed(int64_t tokens, const void *ids, int32_t id_bytes, int64_t rows, int32_t dim,
+                     const void *table, int64_t stride, kbc_type type, float scale, void *out,
+                     void *stream) {
+  if (bad_sizes(tokens, 0, rows, dim, id_bytes) || bad_type(type) || !table || stride < dim)
+    return KBC_EINVAL;
+  if (tokens == 0) return KBC_OK;
+  if (!ids || !out) return KBC_EINVAL;
+  const int per_block = kThreads / group_lanes(type, dim) * kLookupRows;
+  if (ceil_div(tokens, per_block) > kMostBlocks) return KBC_EINVAL;
+  const LookupArgs a{{ids, id_bytes}, tokens, rows, dim, table, stride, scale, out};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  with_rows(type, dim, [&](auto t, auto vec, auto lanes) {
+    using T = decltype(t);
+    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
+    const dim3 grid((unsigned)ceil_div(tokens, kThreads / L * kLookupRows));
+    hipLaunchKernelGGL((lookup_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
+  });
+  return launched();
+}
+
+size_t kbc_embed_pool_scratch_size(int64_t tokens, int64_t bags, int32_t ragged, int32_t dim,
+                                   kbc_type type, int32_t mean) {
+  if (bad_sizes(tokens, bags, 1, dim, 4) || bad_type(type) || bags < 1 ||
+      pools_directly(tokens, bags, ragged != 0))
+    return 0;
+  return scratch_for(tokens, bags, dim, false, mean != 0, group_lanes(type, dim)).bytes;
+}
+
+kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int64_t bags,
+                          const void *offsets, int64_t rows, int32_t dim, const void *table,
+                          int64_t stride, kbc_type type, float scale, int32_t mean, void *out,
+                          void *scratch, size_t bytes, void *stream) {
+  if (bad_sizes(tokens, bags, rows, dim, id_bytes) || bad_type(type) || !table || stride < dim ||
+      (!offsets && bags > 0 && tokens % bags != 0))
+    return KBC_EINVAL;
+  if (bags == 0) return KBC_OK;
+  if ((tokens > 0 && !ids) || !out) return KBC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const Bags of = bags_of(bags, offsets, id_bytes, tokens);
+  if (pools_directly(tokens, bags, offsets != nullptr)) {
+    const PoolArgs a{{ids, id_bytes}, of, rows, dim, mean, table, stride, scale, out};
+    with_rows(type, dim, [&](auto t, auto vec, auto lanes) {
+      using T = decltype(t);
+      constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
+      const dim3 grid((unsigned)bags, (unsigned)ceil_div(dim, L * V));
+      hipLaunchKernelGGL((pool_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
+    });
+    return launched();
+  }
+  const int lpg = group_lanes(type, dim);
+  const Scratch at = scratch_for(tokens, bags, dim, false, mean != 0, lpg);
+  if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
+  char *w = static_cast<char *>(scratch);
+  ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, reinterpret_cast<double *>(w + at.weights),
+             out, bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0};
+  const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads));
+  hipLaunchKernelGGL(pool_list_kernel, grid, dim3(kThreads), 0, s, l);
+  const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), table, stride, dim, nullptr,
+                  mean ? l.weights : nullptr, scale, out, bags,
+                  reinterpret_cast<double *>(w + at.slots)};
+  launch_sum(type, a, s);
+  return launched();
+}
+
+size_t kbc_embed_backward_scratch_size(int64_t tokens, int64_t bags, int32_t dim, kbc_type type,
+                                       int32_t mean) {
+  if (bad_sizes(tokens, bags, 1, dim, 4) || bad_type(type)) return 0;
+  return scratch_for(tokens, bags, dim, true, mean != 0 && bags > 0, group_lanes(type, dim)).bytes;
+}
+
+kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes, int64_t bags,
+                              const void *offsets, int64_t rows, int32_t dim, const void *dout,
+                              kbc_type type, float scale, int32_t mean, void *dtable,
+                              void *scratch, size_t bytes, void *stream) {
+  if (bad_sizes(tokens, bags, rows, dim, id_bytes) || bad_type(type) || !dtable ||
+      (!offsets && bags > 0 && tokens % bags != 0))
+    return KBC_EINVAL;
+  if (tokens > 0 && (!ids || !dout)) return KBC_EINVAL;
+  const int lpg = group_lanes(type, dim);
+  mean = mean && bags > 0;
+  const Scratch at = scratch_for(tokens, bags, dim, true, mean != 0, lpg);
+  if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char *w = static_cast<char *>(scratch);
+  ListArgs l{{ids, id_bytes}, bags_of(bags, offsets, id_bytes, tokens), tokens, rows, mean,
+             reinterpret_cast<double *>(w + at.weights), dtable, rows * dim * size_of(type),
+             reinterpret_cast<int2 *>(w + at.entries), 0, 0};
+  if (tokens <= kRankTokens) {
+    const dim3 grid = list_grid(&l, ceil_div(tokens, kRankPer));
+    hipLaunchKernelGGL(rank_kernel, grid, dim3(kThreads), (size_t)ceil_div(tokens, 4) * 16, s, l);
+  } else {
+    int bits = 1;
+    while ((rows >> bits) != 0) ++bits;  // keys are 0 .. rows
+    const int passes = (int)ceil_div(bits, kDigitBits);
+    RadixArgs r{l, nullptr, nullptr, 0, 0, (uint32_t)ceil_div(tokens, kTile),
+                reinterpret_cast<uint32_t *>(w + at.counts),
+                reinterpret_cast<uint32_t *>(w + at.totals)};
+    int2 *to[2] = {l.entries, reinterpret_cast<int2 *>(w + at.sorted)};
+    for (int p = 0; p < passes; ++p) {
+      r.bits = (bits - r.shift + (passes - p) - 1) / (passes - p);
+      r.out = to[(passes - 1 - p) % 2];  // the last pass writes the entries
+      dim3 grid(r.tiles);
+      r.list.list_wgs = r.tiles;
+      if (p == 0) grid = list_grid(&r.list, r.tiles);
+      hipLaunchKernelGGL(radix_count_kernel, grid, dim3(kThreads), 0, s, r);
+      hipLaunchKernelGGL(radix_scan_kernel, dim3(1u << r.bits), dim3(kThreads), 0, s, r.tiles,
+                         r.counts, r.totals);
+      hipLaunchKernelGGL(radix_place_kernel, dim3(r.tiles), dim3(kThreads), 0, s, r);
+      r.in = r.out;
+      r.shift += r.bits;
+    }
+  }
+  if (tokens > 0) {
+    const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), dout, dim, dim,
+                    mean ? l.weights : nullptr, nullptr, scale, dtable, rows,
+                    reinterpret_cast<double *>(w + at.slots)};
+    launch_sum(type, a, s);
+  }
+  return launched();
+}
+
+}  // extern "C"
