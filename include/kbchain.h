@@ -141,6 +141,50 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
                               kbc_type type, float scale, int32_t mean, void *dtable,
                               void *scratch, size_t bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Penalties, biases and masks on logits
+ * ------------------------------------------------------------------------
+ *
+ * What a column of logits z [n][b] may still take, before its softmax: relations
+ * or words that it has had already are made less likely, biases are added, what a
+ * type, a grammar or a question rules out is masked.  With c the number of times
+ * row i is in column beta's history:
+ *   v = z[i][beta]
+ *   c > 0:  v = v > 0 ? v / repeat : v * repeat;  v -= presence + frequency * c
+ *   v += bias
+ *   not allowed:  v = fill, whatever z holds there
+ */
+typedef struct {
+  const float *bias;      /* DEVICE [n], or [n][b] with bias_each; NULL: none */
+  const void *allowed;    /* DEVICE bytes (0: not allowed), or with allowed_bits 32-bit words, of
+                             which bit i % 32 of word i / 32 is row i's: [rows], or [rows][b] with
+                             allowed_each (rows: n, or words, ceil(n / 32)); NULL: all */
+  int32_t bias_each, allowed_bits, allowed_each;
+  int32_t id_bytes;       /* of history and offsets: 4 (int32) or 8 (int64) */
+  int64_t entries;        /* ids in all histories, at most 2^30; 0: none */
+  const void *history;    /* DEVICE ids; those outside [0, n) are padding */
+  const void *offsets;    /* DEVICE [b + 1], not decreasing: column beta's are [offsets[beta],
+                             offsets[beta + 1]); NULL: entries / b of each column */
+  const float *repeat, *presence, *frequency; /* DEVICE [b], one a column, or NULL: */
+  float repeat_all, presence_all, frequency_all; /* for all columns (none: 1, 0, 0) */
+} kbc_limits;
+
+/* out [n][b], float, of logits z [n][b] of `type`; out must not overlap z.  Every
+ * element is rounded to float once, n < 2^31 - 1.  KBC_EINVAL also where a penalty of
+ * all columns is not finite or repeat_all not positive (a column's own repeat has to
+ * be positive too; it is not checked). */
+kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, const kbc_limits *l,
+                         float fill, float *out, void *stream);
+
+/* Gradients for the upstream gradient dout [n][b]: dz [n][b] of `type`,
+ *   dz = not allowed ? 0 : dout * (c > 0 ? (z > 0 ? 1 / repeat : repeat) : 1),
+ * and unless NULL dbias, [n][b] with bias_each, else [n], summed over the columns in
+ * double, in a fixed order.  z may be NULL where no repeat is given.  The outputs
+ * must not overlap each other or any input. */
+kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type type,
+                                  const kbc_limits *l, const float *dout, void *dz, float *dbias,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -115,7 +115,7 @@ def fingerprint(defines, path, bdir, csrc=CSRC) -> dict:
 CHAIN_LIB = os.path.join(OUT_DIR, "libkbchain.so")
 
 
-CHAIN_SOURCES = ["chain_glue.hip", "embed.hip"]
+CHAIN_SOURCES = ["chain_glue.hip", "embed.hip", "constrain.hip"]
 
 
 def build_chain(verbose: bool = False) -> str:
@@ -123,7 +123,7 @@ def build_chain(verbose: bool = False) -> str:
     shared library."""
     os.makedirs(OUT_DIR, exist_ok=True)
     tmp = CHAIN_LIB + ".tmp"
-    cmd = [hipcc(), "-x", "hip", *DEVICE_FLAGS, *COMMON_FLAGS, "-shared",
+    cmd = [hipcc(), "-x", "hip", *DEVICE_FLAGS, *COMMON_FLAGS, "-I", CSRC, "-shared",
            *[os.path.join(CSRC, f) for f in CHAIN_SOURCES], "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)

@@ -8,8 +8,9 @@ per example), as for the follow operation; reductions run in double on the
 GPU.  Argument marshalling only: every step runs in the library's kernels.
 
 Before the hops stand the question's words: embed() looks up rows of a table,
-scaled, one a token or pooled per question.  It is differentiable; its gradient
-is embed_backward().
+scaled, one a token or pooled per question.  Before a softmax, constrain() applies
+penalties, biases and masks to logits.  Both are differentiable; their gradients
+are embed_backward() and constrain_backward().
 """
 from __future__ import annotations
 
@@ -53,8 +54,21 @@ _lib.kbc_embed_backward_scratch_size.argtypes = [_I64, _I64, _I32, _I32, _I32]
 _lib.kbc_embed_backward_scratch_size.restype = _SZ
 _lib.kbc_embed_backward.argtypes = [_I64, _P, _I32, _I64, _P, _I64, _I32, _P, _I32, _F32, _I32,
                                     _P, _P, _SZ, _P]
+
+
+class _Limits(ctypes.Structure):
+    _fields_ = [("bias", _P), ("allowed", _P), ("bias_each", _I32), ("allowed_bits", _I32),
+                ("allowed_each", _I32), ("id_bytes", _I32), ("entries", _I64), ("history", _P),
+                ("offsets", _P), ("repeat", _P), ("presence", _P), ("frequency", _P),
+                ("repeat_all", _F32), ("presence_all", _F32), ("frequency_all", _F32)]
+
+
+_LIMITS = ctypes.POINTER(_Limits)
+_lib.kbc_constrain.argtypes = [_I64, _I32, _P, _I32, _LIMITS, _F32, _P, _P]
+_lib.kbc_constrain_backward.argtypes = [_I64, _I32, _P, _I32, _LIMITS, _P, _P, _P, _P]
 for _f in (_softmax, _softmax_backward, _l1_normalize, _l1_normalize_backward, _softmax_xent,
-           _lib.kbc_embed, _lib.kbc_embed_pool, _lib.kbc_embed_backward):
+           _lib.kbc_embed, _lib.kbc_embed_pool, _lib.kbc_embed_backward, _lib.kbc_constrain,
+           _lib.kbc_constrain_backward):
     _f.restype = ctypes.c_int
 
 
@@ -301,7 +315,30 @@ def _make_functions():
             return (embed_backward(dout.to(dtype).contiguous(), ids, rows, offsets, scale, pool),
                     None, None, None, None)
 
-    return {"embed": Embed}
+    class Constrain(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
+            out = _constrain_forward(z, bias, allowed, history, offsets, repeat, presence,
+                                     frequency, fill)
+            each = isinstance(repeat, torch.Tensor)
+            scaled = history is not None and (each or repeat != 1.0)
+            ctx.save_for_backward(z if scaled else None, allowed, history if scaled else None,
+                                  offsets, repeat if each else None)
+            ctx.args = z.dtype, None if each else repeat, None if bias is None else bias.dim()
+            return out
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dout):
+            z, allowed, history, offsets, repeat = ctx.saved_tensors
+            dtype, repeat_all, bias_dims = ctx.args
+            dz, dbias = constrain_backward(
+                dout.contiguous(), z, allowed, history, None if history is None else offsets,
+                repeat_all if repeat is None else repeat,
+                bias_dims if ctx.needs_input_grad[1] else None, dtype)
+            return dz, dbias, None, None, None, None, None, None, None
+
+    return {"embed": Embed, "constrain": Constrain}
 
 
 def embed(table, ids, offsets=None, scale=1.0, pool=None):
@@ -318,3 +355,122 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
         return _function("embed").apply(table, ids, offsets, scale, pool)
     return _embed_forward(table, ids, offsets, scale, pool)
+
+
+# -- penalties, biases and masks on logits ----------------------------------------
+
+def _limits(n, b, device, bias, allowed, history, offsets, penalties):
+    """The library's description of what is asked of [n][b] logits on `device`."""
+    import torch
+    l = _Limits(repeat_all=1.0)
+    if bias is not None:
+        if not isinstance(bias, torch.Tensor) or bias.dtype != torch.float32 or \
+                bias.device != device:
+            raise TypeError(f"bias must be a float32 tensor on {device}")
+        if tuple(bias.shape) not in ((n,), (n, b)) or not bias.is_contiguous():
+            raise ValueError(f"bias must be contiguous, of shape {(n,)} or {(n, b)}")
+        l.bias, l.bias_each = bias.data_ptr(), bias.dim() == 2
+    if allowed is not None:
+        if not isinstance(allowed, torch.Tensor) or allowed.device != device or \
+                allowed.dtype not in (torch.bool, torch.int32):
+            raise TypeError(f"allowed must be a bool tensor, or int32 words, on {device}")
+        l.allowed_bits = allowed.dtype == torch.int32
+        rows = (n + 31) // 32 if l.allowed_bits else n
+        if tuple(allowed.shape) not in ((rows,), (rows, b)) or not allowed.is_contiguous():
+            raise ValueError(f"allowed must be contiguous, of shape {(rows,)} or {(rows, b)}")
+        l.allowed, l.allowed_each = allowed.data_ptr(), allowed.dim() == 2
+    if history is None:
+        if offsets is not None:
+            raise ValueError("offsets go with a history")
+        return l
+    columns, l.offsets = _bag_args(history, offsets, "sum", device)
+    if columns != b:
+        raise ValueError(f"history must be of {b} columns")
+    l.history, l.entries, l.id_bytes = history.data_ptr(), history.numel(), history.element_size()
+    for name, value in penalties.items():
+        if isinstance(value, torch.Tensor):
+            if value.dtype != torch.float32 or value.device != device:
+                raise TypeError(f"{name} must be a number or a float32 tensor on {device}")
+            if tuple(value.shape) != (b,) or not value.is_contiguous():
+                raise ValueError(f"{name} must be a number or a contiguous [{b}] tensor")
+            setattr(l, name, value.data_ptr())
+        else:
+            value = float(value)
+            if not -3.0e38 < value < 3.0e38 or (name == "repeat" and value <= 0.0):
+                raise ValueError(f"{name} must be finite, and repeat positive")
+            setattr(l, name + "_all", value)
+    return l
+
+
+def _logits(z, name):
+    """(rows, columns, type code) of logits."""
+    code = _type(z, name)
+    if z.dim() != 2 or z.shape[0] < 1 or z.shape[1] < 1 or not z.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [n][b] tensor, not empty")
+    return z.shape[0], z.shape[1], code
+
+
+def _constrain_forward(z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
+    import torch
+    n, b, code = _logits(z, "z")
+    l = _limits(n, b, z.device, bias, allowed, history, offsets,
+                {"repeat": repeat, "presence": presence, "frequency": frequency})
+    out = torch.empty((n, b), dtype=torch.float32, device=z.device)
+    _run(_lib.kbc_constrain, "kbc_constrain", z.device, n, b, z.data_ptr(), code, l, float(fill),
+         out.data_ptr())
+    return out
+
+
+def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0, presence=0.0,
+              frequency=0.0, fill=float("-inf")):
+    """Logits z [n][b] (float32, bfloat16 or float16) with penalties, biases and a mask
+    applied, float32 [n][b].  With c the number of times row i is in its column's
+    history:
+
+      v = z;  where c > 0: v = v / repeat if v > 0 else v * repeat, then
+      v -= presence + frequency * c;  v += bias;  where not allowed: v = fill
+
+    bias: float32 [n] or [n][b].  allowed: bool [n] or [n][b], or int32 words, bit
+    i % 32 of word i // 32 row i's: [ceil(n / 32)] or [ceil(n / 32)][b].  history: ids,
+    one row a column of a 2-D tensor, or 1-D with offsets (b + 1 of them, not
+    decreasing, of the ids' type); ids outside [0, n) are padding.  repeat (positive),
+    presence, frequency: numbers, or float32 [b], one a column.  A column that nothing
+    is left to is `fill` throughout: chain.softmax makes NaN of it where fill is -inf,
+    equal parts where it is finite; chain.softmax_xent wants a finite fill.
+    Differentiable with respect to z and bias.
+    """
+    import torch
+    args = (z, bias, allowed, history, offsets, repeat, presence, frequency, fill)
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
+                                       for t in (z, bias)):
+        return _function("constrain").apply(*args)
+    return _constrain_forward(*args)
+
+
+def constrain_backward(dout, z=None, allowed=None, history=None, offsets=None, repeat=1.0,
+                       bias_dims=None, dtype=None):
+    """(dz, dbias) of constrain for the upstream gradient dout [n][b]: dz of z's type
+    (dtype's where z is not given; z is needed where a history has a repeat), dbias
+    None, or with bias_dims 1 or 2 that of a bias [n] or [n][b]."""
+    import torch
+    dout = _mat(dout, "dout")
+    device = dout.device
+    n, b = dout.shape
+    if z is not None:
+        if _logits(z, "z")[:2] != (n, b) or z.device != device:
+            raise ValueError(f"z must be a contiguous {(n, b)} tensor on {device}")
+        dtype = z.dtype
+    if bias_dims not in (None, 1, 2):
+        raise ValueError("bias_dims must be None, 1 or 2")
+    dz = torch.empty((n, b), dtype=dtype or torch.float32, device=device)
+    code = _type(dz, "dz")
+    l = _limits(n, b, device, None, allowed, history, offsets, {"repeat": repeat})
+    l.bias_each = bias_dims == 2
+    dbias = None if bias_dims is None else \
+        torch.empty((n,) if bias_dims == 1 else (n, b), dtype=torch.float32, device=device)
+    if l.entries and (l.repeat or l.repeat_all != 1.0) and z is None:
+        raise ValueError("z is needed where a history has a repeat")
+    _run(_lib.kbc_constrain_backward, "kbc_constrain_backward", device, n, b,
+         None if z is None else z.data_ptr(), code, l, dout.data_ptr(), dz.data_ptr(),
+         None if dbias is None else dbias.data_ptr())
+    return dz, dbias

@@ -1,0 +1,375 @@
+// constrain.hip -- penalties for what a column has had, biases and masks on logits
+// (kbchain.h: kbc_constrain, kbc_constrain_backward).
+//
+// Element (i, beta) of an [n][b] array, c the number of times i is in column
+// beta's history:
+//     v = z;  c > 0:  v = v > 0 ? v / repeat : v * repeat,
+//                     v -= presence + frequency * c
+//     v += bias;  not allowed:  v = fill
+// and the gradient:  not allowed: 0, else dz = dout * (c > 0 ? (z > 0 ? 1 / repeat :
+// repeat) : 1), dbias = dout.
+//
+// One pass over the arrays in the order they lie in, 4 elements a lane, writes every
+// element as if no history were, bound by the bytes it moves; then the few elements
+// of the history are written again, by the threads that count them.  (A dense array
+// of counts would be read and written as a whole for them.)  A column's ids are
+// compared with each other, a block of them in LDS at a time: no table that ids
+// could overflow, nothing to clear, and an id that occurs twice is written twice
+// with the same value.  A shared bias' gradient is summed row by row, in double, in
+// a fixed order, by the lanes that write the row.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "ids.h"
+#include "kbchain.h"
+
+namespace {
+
+using namespace kbc;
+
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned char uchar4_any __attribute__((ext_vector_type(4), aligned(1)));
+template <class T>
+using vec4_any = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+
+enum Allowed { kAll, kBytes, kBits };
+
+struct Args {
+  int64_t n;
+  int32_t b;
+  uint32_t magic;  // ceil(2^32 / b), for b <= kTile
+  const void *z;   // logits (forward), or null
+  const float *dout;
+  const float *bias;
+  int32_t bias_each;
+  const void *allowed;
+  int32_t allowed_kind, allowed_each;
+  float fill;
+  void *out;       // float (forward), dz of the logits' type (backward)
+  float *dbias;
+};
+
+__device__ __forceinline__ bool is_allowed(const Args &a, int64_t i, int32_t col) {
+  if (a.allowed_kind == kAll) return true;
+  if (a.allowed_kind == kBytes)
+    return static_cast<const uint8_t *>(a.allowed)[a.allowed_each ? i * a.b + col : i] != 0;
+  const uint32_t *w = static_cast<const uint32_t *>(a.allowed);
+  return w[a.allowed_each ? (i >> 5) * a.b + col : i >> 5] >> (i & 31) & 1;
+}
+__device__ __forceinline__ float bias_of(const Args &a, int64_t i, int32_t col) {
+  return a.bias ? a.bias[a.bias_each ? i * a.b + col : i] : 0.0f;
+}
+
+// -- every element, as if no history were ---------------------------------------------
+
+constexpr int kDepth = 4;                      // vectors of 4 elements of a thread
+constexpr int kTile = kThreads * 4 * kDepth;   // elements of a workgroup
+
+// BACKWARD: dz (and a bias' own gradient, one an element) from dout.
+template <class T, bool BACKWARD>
+__global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
+  using In = std::conditional_t<BACKWARD, float, T>;
+  using Out = std::conditional_t<BACKWARD, T, float>;
+  const In *in = BACKWARD ? reinterpret_cast<const In *>(a.dout) : static_cast<const In *>(a.z);
+  Out *out = static_cast<Out *>(a.out);
+  const int64_t first = (int64_t)blockIdx.x * kTile, size = a.n * a.b;
+  const int64_t row0 = first / a.b;
+  const uint32_t rest = (uint32_t)(first - row0 * a.b);
+  vec4_any<In> v[kDepth];
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) {
+    const int64_t f = first + (k * kThreads + (int)threadIdx.x) * 4;
+    if (f + 4 <= size) {
+      v[k] = *reinterpret_cast<const vec4_any<In> *>(in + f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[k][e] = f + e < size ? in[f + e] : (In)0.0f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kDepth; ++k) {
+    const uint32_t local = (uint32_t)(k * kThreads + (int)threadIdx.x) * 4;
+    const int64_t f = first + local;
+    if (f >= size) break;
+    // The row and column of the first of the four: exact, as the dividend is
+    // below 2 b where b is above kTile, and below 2 kTile where it is not.
+    const uint32_t x = rest + local;
+    const uint32_t q = a.b > kTile ? (uint32_t)(x >= (uint32_t)a.b) : a.b == 1 ? x : __umulhi(x, a.magic);
+    int64_t i = row0 + q;
+    int32_t col = (int32_t)(x - q * (uint32_t)a.b);
+    float y[4];
+    bool ok[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool in_range = f + e < size;
+      ok[e] = in_range && is_allowed(a, i, col);
+      y[e] = (float)v[k][e];
+      if constexpr (BACKWARD) {
+        y[e] = ok[e] ? y[e] : 0.0f;
+      } else {
+        if (in_range) y[e] += bias_of(a, i, col);
+        y[e] = ok[e] ? y[e] : a.fill;
+      }
+      if (++col == a.b) {
+        col = 0;
+        ++i;
+      }
+    }
+    if (f + 4 <= size) {
+      vec4_any<Out> o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (Out)y[e];
+      __builtin_nontemporal_store(o, reinterpret_cast<vec4_any<Out> *>(out + f));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f + e < size) out[f + e] = (Out)y[e];
+    }
+    if constexpr (BACKWARD)
+      if (a.dbias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (f + e < size) a.dbias[f + e] = y[e];
+      }
+  }
+}
+
+// The backward pass with a shared bias: G lanes a row, which they also sum.
+template <class T, int G>
+__global__ __launch_bounds__(kThreads) void row_kernel(Args a) {
+  const int lane = threadIdx.x % G;
+  const int64_t i = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  if (i >= a.n) return;  // whole groups; their shuffles stay inside the group
+  const float *g = a.dout + i * a.b;
+  T *dz = static_cast<T *>(a.out) + i * a.b;
+  double sum = 0.0;
+  for (int64_t c = lane * 4; c < a.b; c += G * 4) {
+    const int m = (int)min((int64_t)4, a.b - c);
+    float v[4];
+    if (m == 4) {
+      const float4_any t = *reinterpret_cast<const float4_any *>(g + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = t[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = e < m ? g[c + e] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = e < m && is_allowed(a, i, (int32_t)(c + e)) ? v[e] : 0.0f;
+      sum += (double)v[e];
+    }
+    if (m == 4) {
+      vec4_any<T> o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (T)v[e];
+      __builtin_nontemporal_store(o, reinterpret_cast<vec4_any<T> *>(dz + c));
+    } else {
+      for (int e = 0; e < m; ++e) dz[c + e] = (T)v[e];
+    }
+  }
+#pragma unroll
+  for (int m = 1; m < G; m <<= 1) sum += __shfl_xor(sum, m);
+  if (lane == 0) a.dbias[i] = (float)sum;
+}
+
+// -- the elements of the history --------------------------------------------------------
+
+struct Penalties {
+  Ints ids;
+  Bags columns;
+  const float *repeat, *presence, *frequency;  // [b], or null:
+  float repeat_all, presence_all, frequency_all;
+};
+
+constexpr int kEntryLanes = 8;                       // lanes that share an entry's count
+constexpr int kEntries = kThreads / kEntryLanes;     // entries of a workgroup
+constexpr int kBlockIds = 2048;                      // ids in LDS at a time
+
+template <class T, bool BACKWARD>
+__global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) {
+  __shared__ int4 lds[kBlockIds / 4];
+  __shared__ int64_t range[2];
+  int *ids = reinterpret_cast<int *>(lds);
+  const int lane = threadIdx.x % kEntryLanes;
+  const int64_t t0 = (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / kEntryLanes;
+  const int64_t total = p.columns.tokens;
+  const int64_t col = t < total ? bag_of(p.columns, t) : -1;
+  int64_t id = -1, begin = 0, end = 0;
+  if (col >= 0) {
+    id = load_int(p.ids, t);
+    if (id >= a.n) id = -1;
+    begin = bag_begin(p.columns, col);
+    end = bag_begin(p.columns, col + 1);
+  }
+  const bool valid = id >= 0;  // the same for the lanes of an entry
+  const bool counts = !BACKWARD && (p.frequency || p.frequency_all != 0.0f);
+  int count = 0;
+  if (counts) {  // uniform
+    // The ids of every column that the workgroup's entries are of.
+    if (threadIdx.x == 0) {
+      const int64_t c0 = bag_of(p.columns, t0);
+      const int64_t c1 = bag_of(p.columns, min(t0 + kEntries, total) - 1);
+      range[0] = c0 < 0 ? t0 : bag_begin(p.columns, c0);
+      range[1] = c1 < 0 ? t0 + kEntries : bag_begin(p.columns, c1 + 1);
+    }
+    __syncthreads();
+    const int64_t r1 = min(range[1], total);
+    for (int64_t r0 = range[0]; r0 < r1; r0 += kBlockIds) {
+      __syncthreads();  // the block before has been read
+      for (int k = threadIdx.x; k < kBlockIds; k += kThreads) {
+        const int64_t x = r0 + k < r1 ? load_int(p.ids, r0 + k) : -1;
+        ids[k] = x >= 0 && x < a.n ? (int)x : -1;
+      }
+      __syncthreads();
+      if (valid) {
+        const int lo = (int)max((int64_t)0, begin - r0);
+        const int hi = (int)min((int64_t)kBlockIds, end - r0);
+        for (int q = lo / 4 + lane; q * 4 < hi; q += kEntryLanes) {
+          const int4 x = lds[q];
+          if (q * 4 >= lo && q * 4 + 4 <= hi) {
+            count += (x.x == id) + (x.y == id) + (x.z == id) + (x.w == id);
+          } else {
+            const int at = q * 4;
+            count += (x.x == id && at >= lo && at < hi) + (x.y == id && at + 1 >= lo && at + 1 < hi) +
+                     (x.z == id && at + 2 >= lo && at + 2 < hi) +
+                     (x.w == id && at + 3 >= lo && at + 3 < hi);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 1; m < kEntryLanes; m <<= 1) count += __shfl_xor(count, m);
+  }
+  if (!valid || lane != 0) return;
+  const int64_t f = id * a.b + col;
+  const bool ok = is_allowed(a, id, (int32_t)col);
+  const double repeat = p.repeat ? p.repeat[col] : p.repeat_all;
+  const double z = (double)(float)static_cast<const T *>(a.z)[f];
+  if constexpr (BACKWARD) {
+    const double g = a.dout[f];
+    static_cast<T *>(a.out)[f] = (T)(ok ? (float)(z > 0.0 ? g / repeat : g * repeat) : 0.0f);
+  } else {
+    double v = z > 0.0 ? z / repeat : z * repeat;
+    v -= p.presence ? p.presence[col] : p.presence_all;
+    if (counts) v -= (double)(p.frequency ? p.frequency[col] : p.frequency_all) * count;
+    v += (double)bias_of(a, id, (int32_t)col);
+    static_cast<float *>(a.out)[f] = ok ? (float)v : a.fill;
+  }
+}
+
+// -- how a call is launched ----------------------------------------------------------------
+
+template <class F>
+void with_type(kbc_type type, F f) {
+  switch (type) {
+    case KBC_F32: f(float{}); break;
+    case KBC_BF16: f(__bf16{}); break;
+    case KBC_F16: f(_Float16{}); break;
+  }
+}
+
+bool bad_limits(int64_t n, int32_t b, kbc_type type, const kbc_limits *l) {
+  if (n < 1 || n > kMostRows || b < 1 || bad_type(type) || !l) return true;
+  if (ceil_div(n * b, kTile) > kMostBlocks || ceil_div(n, 4) > kMostBlocks) return true;
+  if (l->entries < 0 || l->entries > kMostTokens) return true;
+  if (l->entries > 0) {
+    if (!l->history || (l->id_bytes != 4 && l->id_bytes != 8)) return true;
+    if (!l->offsets && l->entries % b != 0) return true;
+  }
+  auto bad = [](float x) { return !std::isfinite(x); };
+  return bad(l->repeat_all) || bad(l->presence_all) || bad(l->frequency_all) ||
+         (!l->repeat && !(l->repeat_all > 0.0f));
+}
+
+Args args_for(int64_t n, int32_t b, const kbc_limits *l) {
+  Args a{};
+  a.n = n;
+  a.b = b;
+  a.magic = (uint32_t)((((uint64_t)1 << 32) + b - 1) / b);
+  a.bias = l->bias;
+  a.bias_each = l->bias_each;
+  a.allowed = l->allowed;
+  a.allowed_kind = !l->allowed ? kAll : l->allowed_bits ? kBits : kBytes;
+  a.allowed_each = l->allowed_each;
+  return a;
+}
+Penalties penalties_for(int32_t b, const kbc_limits *l) {
+  return {{l->history, l->id_bytes}, bags_of(b, l->offsets, l->id_bytes, l->entries),
+          l->repeat, l->presence, l->frequency, l->repeat_all, l->presence_all, l->frequency_all};
+}
+
+template <class T, int G>
+void launch_rows(const Args &a, hipStream_t s) {
+  hipLaunchKernelGGL((row_kernel<T, G>), dim3((unsigned)ceil_div(a.n, kThreads / G)),
+                     dim3(kThreads), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, const kbc_limits *l,
+                         float fill, float *out, void *stream) {
+  if (bad_limits(n, b, type, l) || !z || !out) return KBC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Args a = args_for(n, b, l);
+  a.z = z;
+  a.fill = fill;
+  a.out = out;
+  const bool penalised = l->entries > 0 && (l->repeat || l->presence || l->frequency ||
+                                            l->repeat_all != 1.0f || l->presence_all != 0.0f ||
+                                            l->frequency_all != 0.0f);
+  with_type(type, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL((dense_kernel<T, false>), dim3((unsigned)ceil_div(n * b, kTile)),
+                       dim3(kThreads), 0, s, a);
+    if (penalised)
+      hipLaunchKernelGGL((history_kernel<T, false>), dim3((unsigned)ceil_div(l->entries, kEntries)),
+                         dim3(kThreads), 0, s, a, penalties_for(b, l));
+  });
+  return launched();
+}
+
+kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type type,
+                                  const kbc_limits *l, const float *dout, void *dz, float *dbias,
+                                  void *stream) {
+  if (bad_limits(n, b, type, l) || !dout || !dz) return KBC_EINVAL;
+  const bool scaled = l->entries > 0 && (l->repeat || l->repeat_all != 1.0f);
+  if (scaled && !z) return KBC_EINVAL;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Args a = args_for(n, b, l);
+  a.z = z;
+  a.dout = dout;
+  a.out = dz;
+  a.dbias = dbias;
+  with_type(type, [&](auto t) {
+    using T = decltype(t);
+    if (dbias && !l->bias_each) {
+      if (b <= 8)
+        launch_rows<T, 2>(a, s);
+      else if (b <= 16)
+        launch_rows<T, 4>(a, s);
+      else if (b <= 32)
+        launch_rows<T, 8>(a, s);
+      else if (b <= 64)
+        launch_rows<T, 16>(a, s);
+      else if (b <= 128)
+        launch_rows<T, 32>(a, s);
+      else
+        launch_rows<T, 64>(a, s);
+    } else {
+      hipLaunchKernelGGL((dense_kernel<T, true>), dim3((unsigned)ceil_div(n * b, kTile)),
+                         dim3(kThreads), 0, s, a);
+    }
+    if (scaled)
+      hipLaunchKernelGGL((history_kernel<T, true>), dim3((unsigned)ceil_div(l->entries, kEntries)),
+                         dim3(kThreads), 0, s, a, penalties_for(b, l));
+  });
+  return launched();
+}
+
+}  // extern "C"

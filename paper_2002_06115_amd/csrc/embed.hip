@@ -28,12 +28,12 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "ids.h"
 #include "kbchain.h"
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWave = 64;
+using namespace kbc;
 
 // -- rows of a type ---------------------------------------------------------------
 
@@ -66,42 +66,6 @@ __device__ __forceinline__ void store_vals(T *p, const T (&v)[VEC]) {
     for (int k = 0; k < VEC; ++k) t[k] = v[k];
     __builtin_nontemporal_store(t, reinterpret_cast<typename Row<T>::vec *>(p));
   }
-}
-
-// The ids and offsets of a call, int32 or int64.
-struct Ints {
-  const void *p;
-  int bytes;
-};
-__device__ __forceinline__ int64_t load_int(const Ints &a, int64_t i) {
-  return a.bytes == 8 ? static_cast<const int64_t *>(a.p)[i]
-                      : (int64_t)static_cast<const int32_t *>(a.p)[i];
-}
-
-// How tokens are grouped into bags: bag g holds tokens [begin(g), begin(g + 1)).
-struct Bags {
-  int64_t n;       // 0: every token is an output row of its own
-  Ints offsets;    // null: n bags of `each` tokens
-  int64_t each;
-  int64_t tokens;
-};
-__device__ __forceinline__ int64_t bag_begin(const Bags &b, int64_t g) {
-  if (!b.offsets.p) return g * b.each;
-  const int64_t o = load_int(b.offsets, g);
-  return o < 0 ? 0 : o > b.tokens ? b.tokens : o;  // never a token past the last
-}
-// The bag of token t, -1 where it is in none.
-__device__ __forceinline__ int64_t bag_of(const Bags &b, int64_t t) {
-  if (!b.offsets.p) return t / b.each;
-  int64_t lo = 0, hi = b.n + 1;  // offsets [0, lo) are <= t, [hi, n] are > t
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (bag_begin(b, mid) <= t)
-      lo = mid + 1;
-    else
-      hi = mid;
-  }
-  return lo >= 1 && lo <= b.n ? lo - 1 : -1;
 }
 
 // -- plain lookup -------------------------------------------------------------------
@@ -666,13 +630,6 @@ void with_rows(kbc_type type, int32_t dim, F f) {
   }
 }
 
-int64_t size_of(kbc_type t) { return t == KBC_F32 ? 4 : 2; }
-bool bad_type(kbc_type t) { return t != KBC_F32 && t != KBC_BF16 && t != KBC_F16; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-size_t padded(int64_t bytes) { return (size_t)ceil_div(bytes, 256) * 256; }
-
-kbc_status launched() { return hipGetLastError() == hipSuccess ? KBC_OK : KBC_EHIP; }
-
 // Entries of a chunk: about 4096 waves' worth of lane groups over the list, at
 // least kSumRows entries each.
 int32_t chunk_for(int64_t tokens, int lpg) {
@@ -682,6 +639,7 @@ int32_t chunk_for(int64_t tokens, int lpg) {
 }
 
 // Where a call's scratch holds what.
+size_t padded(int64_t bytes) { return (size_t)ceil_div(bytes, 256) * 256; }
 struct Scratch {
   size_t entries, sorted, counts, totals, weights, slots, bytes;
 };
@@ -712,7 +670,6 @@ int group_lanes(kbc_type type, int32_t dim) {
 
 // A pooled sum takes a workgroup per bag where no bag can be long: few tokens in
 // all, or bags of one, small length.
-constexpr int64_t kMostBlocks = (int64_t(1) << 32) / kThreads - 1;  // a grid's threads fit 32 bits
 bool pools_directly(int64_t tokens, int64_t bags, bool ragged) {
   return bags <= kMostBlocks && (tokens <= 4096 || (!ragged && tokens / bags <= 512));
 }
@@ -741,10 +698,6 @@ dim3 list_grid(ListArgs *a, int64_t list_wgs) {
   return dim3((unsigned)(list_wgs + a->weight_wgs + ceil_div(a->fill_bytes, kFillBytes)));
 }
 
-// A call's sizes: every index into rows, tokens and bags fits an int, and so do
-// the lists' places and grids.
-constexpr int64_t kMostTokens = int64_t(1) << 30;
-constexpr int64_t kMostRows = (int64_t)INT32_MAX - 1;
 bool bad_sizes(int64_t tokens, int64_t bags, int64_t rows, int32_t dim, int32_t id_bytes) {
   return tokens < 0 || tokens > kMostTokens || bags < 0 || bags > kMostRows || rows < 1 ||
          rows > kMostRows || dim < 1 || dim > 65536 || (id_bytes != 4 && id_bytes != 8);
@@ -753,10 +706,6 @@ bool bad_scratch(const Scratch &need, const void *scratch, size_t bytes) {
   return need.bytes > 0 &&
          (!scratch || bytes < need.bytes || reinterpret_cast<uintptr_t>(scratch) % 16 != 0);
 }
-Bags bags_of(int64_t bags, const void *offsets, int32_t id_bytes, int64_t tokens) {
-  return {bags, {offsets, id_bytes}, bags > 0 ? tokens / bags : 1, tokens};
-}
-
 }  // namespace
 
 extern "C" {
