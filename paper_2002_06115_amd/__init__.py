@@ -10,6 +10,7 @@ and the current stream.
     dX, dR = kb.follow_backward(X, R, dY)
     Y  = follow(kb, X, R)                                   # autograd-aware
     Y  = follow_residual(kb, X, R)                          # follow(X, R) + X (App. E)
+    Y  = follow(kb, X, R, pack=True)                        # X kept in 8 bits for the backward
 
 Activations are entity-major and batch-contiguous float32 CUDA tensors:
 ``X[i, beta]`` is the weight of entity i in example beta (the transpose of the
@@ -78,6 +79,16 @@ def _load_library():
     lib.kb_follow_accumulate.restype = ctypes.c_int
     lib.kb_follow_backward_residual.argtypes = [p, i32, p, p, p, f32, p, p, p, sz, p]
     lib.kb_follow_backward_residual.restype = ctypes.c_int
+    lib.kb_packed_pitch.argtypes = [i32]
+    lib.kb_packed_pitch.restype = sz
+    lib.kb_pack.argtypes = [i64, i32, p, p, p, p]
+    lib.kb_pack.restype = ctypes.c_int
+    lib.kb_unpack.argtypes = [i64, i32, p, p, p, p]
+    lib.kb_unpack.restype = ctypes.c_int
+    lib.kb_follow_backward_packed.argtypes = [p, i32, p, p, p, p, p, p, p, sz, p]
+    lib.kb_follow_backward_packed.restype = ctypes.c_int
+    lib.kb_follow_backward_residual_packed.argtypes = [p, i32, p, p, p, p, f32, p, p, p, sz, p]
+    lib.kb_follow_backward_residual_packed.restype = ctypes.c_int
     lib.kb_status_str.argtypes = [ctypes.c_int]
     lib.kb_status_str.restype = ctypes.c_char_p
     lib.kb_last_error.argtypes = []
@@ -149,6 +160,69 @@ def layout_host(subj, rel, obj, n_entities, n_relations, which):
                                _np_ptr(obj), which, _np_ptr(off), _np_ptr(ca), _np_ptr(cb),
                                _np_ptr(perm)), "kb_layout_host")
     return off, ca, cb, perm
+
+
+def _on_device(fn, what, device, *args):
+    """fn(*args, current stream of `device`) with that device current."""
+    import torch
+    raw = torch._C._cuda_getCurrentRawStream(device.index)
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, raw)
+    if status != KB_OK:
+        _check(status, what)
+
+
+class Packed:
+    """Entity sets [rows][b] kept in 8 bits (pack): e4m3 codes and an exponent a row."""
+
+    def __init__(self, codes, exponents, b):
+        import torch
+        for t, name, dims in ((codes, "codes", 2), (exponents, "exponents", 1)):
+            if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_cuda:
+                raise TypeError(f"{name} must be a uint8 CUDA tensor")
+            if t.dim() != dims or not t.is_contiguous() or t.device != codes.device or \
+                    t.shape[0] != codes.shape[0]:
+                raise ValueError("codes and exponents must be contiguous, a row and a byte a set")
+        if b < 1 or codes.shape[1] != _lib.kb_packed_pitch(int(b)):
+            raise ValueError(f"codes are not those of rows of {b} values")
+        self.codes, self.exponents, self.b = codes, exponents, int(b)
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.b
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def unpack(self):
+        """The values kept, float32 [rows][b]."""
+        import torch
+        X = torch.empty(self.shape, dtype=torch.float32, device=self.device)
+        _on_device(_lib.kb_unpack, "kb_unpack", self.device, self.codes.shape[0], self.b,
+                   self.codes.data_ptr(), self.exponents.data_ptr(), X.data_ptr())
+        return X
+
+
+def pack(X):
+    """X [rows][b] kept in 8 bits, a quarter of the memory: row j as 8-bit floats (e4m3,
+    rounded to nearest even) of X[j] / 2^e, e the smallest exponent from -127 on with
+    |x| <= 448 * 2^e for every finite x of the row.  A kept value is off by at most
+    2^-4 of itself, or 2^-10 * 2^e; infinities are kept as NaN."""
+    import torch
+    if not isinstance(X, torch.Tensor) or X.dtype != torch.float32 or not X.is_cuda:
+        raise TypeError("X must be a float32 CUDA tensor")
+    if X.dim() != 2 or X.shape[1] < 1 or not X.is_contiguous():
+        raise ValueError("X must be a contiguous [rows][b] tensor")
+    rows, b = X.shape
+    codes = torch.empty((rows, _lib.kb_packed_pitch(b)), dtype=torch.uint8, device=X.device)
+    exponents = torch.empty(rows, dtype=torch.uint8, device=X.device)
+    _on_device(_lib.kb_pack, "kb_pack", X.device, rows, b, X.data_ptr(), codes.data_ptr(),
+               exponents.data_ptr())
+    return Packed(codes, exponents, b)
 
 
 class KB:
@@ -303,12 +377,17 @@ class KB:
         """(dX [N_E][b], dR [N_R][b]) for upstream gradient dY [N_E][b].
 
         With ``residual=gamma`` the gradients of follow(X, R) + gamma * X
-        (dX gains gamma * dY).
+        (dX gains gamma * dY).  X may be packed (pack): dR is that of the values
+        kept.
         """
         import torch
         dY = self._act(dY, self.n_entities, "dY")
         b = dY.shape[1]
-        X = self._act(X, self.n_entities, "X") if want_dr else None
+        packed = X if isinstance(X, Packed) and want_dr else None
+        if packed is not None and (packed.shape != (self.n_entities, b) or
+                                   packed.device != self.device):
+            raise ValueError(f"X must be packed from [{self.n_entities}][{b}] on {self.device}")
+        X = self._act(X, self.n_entities, "X") if want_dr and packed is None else None
         R = self._act(R, self.n_relations, "R") if want_dx else None
         if want_dx and dX is None:
             dX = torch.empty((self.n_entities, b), dtype=torch.float32, device=self.device)
@@ -316,7 +395,18 @@ class KB:
             dR = torch.empty((self.n_relations, b), dtype=torch.float32, device=self.device)
         dX = self._act(dX, self.n_entities, "dX") if want_dx else None
         dR = self._act(dR, self.n_relations, "dR") if want_dr else None
-        if residual is None:
+        if packed is not None:
+            kept = packed.codes.data_ptr(), packed.exponents.data_ptr()
+            if residual is None:
+                self._enqueue(_lib.kb_follow_backward_packed, "kb_follow_backward_packed", stream,
+                              b, *kept, self._ptr(R), self._ptr(dY), self._ptr(dX),
+                              self._ptr(dR))
+            else:
+                self._enqueue(_lib.kb_follow_backward_residual_packed,
+                              "kb_follow_backward_residual_packed", stream, b, *kept,
+                              self._ptr(R), self._ptr(dY), float(residual), self._ptr(dX),
+                              self._ptr(dR))
+        elif residual is None:
             self._enqueue(_lib.kb_follow_backward, "kb_follow_backward", stream, b, self._ptr(X),
                           self._ptr(R), self._ptr(dY), self._ptr(dX), self._ptr(dR))
         else:
@@ -377,26 +467,56 @@ def _make_functions():
                                             want_dr=need_r, residual=ctx.residual)
             return dX, dR, None, None
 
-    return _Follow
+    class _FollowPacked(torch.autograd.Function):
+        """The same with X kept in 8 bits, where R's gradient will need it."""
+        @staticmethod
+        def forward(ctx, X, R, kb, residual):
+            ctx.kb = kb
+            ctx.residual = residual
+            ctx.b = X.shape[-1]
+            kept = (None, None)
+            if ctx.needs_input_grad[1]:
+                P = pack(X)
+                kept = P.codes, P.exponents
+            ctx.save_for_backward(*kept, R if ctx.needs_input_grad[0] else None)
+            return kb.follow(X, R, residual=residual)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dY):
+            codes, exponents, R = ctx.saved_tensors
+            need_x, need_r = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
+            X = Packed(codes, exponents, ctx.b) if need_r else None
+            dX, dR = ctx.kb.follow_backward(X, R, dY.contiguous(), want_dx=need_x,
+                                            want_dr=need_r, residual=ctx.residual)
+            return dX, dR, None, None
+
+    return _Follow, _FollowPacked
 
 
-_FollowFn = None
+_FollowFns = None
 
 
-def follow(kb: KB, X, R):
-    """Differentiable follow(X, R) (Eq. 4) on entity-major tensors X [N_E][b], R [N_R][b]."""
-    global _FollowFn
-    if _FollowFn is None:
-        _FollowFn = _make_functions()
-    return _FollowFn.apply(X, R, kb, None)
+def _follow_fn(pack):
+    global _FollowFns
+    if _FollowFns is None:
+        _FollowFns = _make_functions()
+    return _FollowFns[1 if pack else 0]
 
 
-def follow_residual(kb: KB, X, R, gamma: float = 1.0):
-    """Differentiable residual hop follow(X, R) + gamma * X (Sec. 3.2, App. E)."""
-    global _FollowFn
-    if _FollowFn is None:
-        _FollowFn = _make_functions()
-    return _FollowFn.apply(X, R, kb, float(gamma))
+def follow(kb: KB, X, R, pack: bool = False):
+    """Differentiable follow(X, R) (Eq. 4) on entity-major tensors X [N_E][b], R [N_R][b].
+
+    With ``pack`` the backward pass keeps X in 8 bits (a quarter of the memory):
+    R's gradient is that of the values kept (see pack()), X's is the same."""
+    return _follow_fn(pack).apply(X, R, kb, None)
 
 
-__all__ = ["KB", "KBError", "follow", "follow_residual", "layout_host", "LIB_PATH", "PHASES"]
+def follow_residual(kb: KB, X, R, gamma: float = 1.0, pack: bool = False):
+    """Differentiable residual hop follow(X, R) + gamma * X (Sec. 3.2, App. E);
+    ``pack`` as for follow."""
+    return _follow_fn(pack).apply(X, R, kb, float(gamma))
+
+
+__all__ = ["KB", "KBError", "Packed", "follow", "follow_residual", "layout_host", "pack",
+           "LIB_PATH", "PHASES"]

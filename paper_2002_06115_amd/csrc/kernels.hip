@@ -806,6 +806,318 @@ __global__ __launch_bounds__(kBlock) void narrow_kernel(StreamArgs a) {
   }
 }
 
+// -- entity sets in 8 bits ------------------------------------------------------
+//
+// The dR pass with X as launch_pack left it: the stream kernel without its
+// residual and LDS forms, a run's B row decoded when it starts,
+//     held = decode(codes[b_id]) * 2^(exponents[b_id] - 127),
+// which is exact (4 significant bits, within a float's range), so dR is the sum over
+// the kept values with one rounding, as from a float X.  The exponents of a step's
+// run starts are read by the lanes that fetched the entries, one load for all, and
+// shared like the entries.
+//
+// LANE: 4 floats per lane, kRaggedLane likewise, or 1 (rows of less than 4 floats).
+
+// The four values of a dword of codes, times 2^e.
+__device__ __forceinline__ void decode4(uint32_t codes, int e, float (&v)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false);
+  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+  v[0] = __builtin_ldexpf(lo[0], e);
+  v[1] = __builtin_ldexpf(lo[1], e);
+  v[2] = __builtin_ldexpf(hi[0], e);
+  v[3] = __builtin_ldexpf(hi[1], e);
+}
+__device__ __forceinline__ float decode1(uint32_t code, int e) {
+  return __builtin_ldexpf(__builtin_amdgcn_cvt_f32_fp8((int)code, 0), e);
+}
+constexpr int kPackBias = 127;
+
+template <int LANE, int LPT, bool BUF, bool WEIGHTED>
+__global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
+  constexpr bool RAGGED = LANE == kRaggedLane;
+  constexpr int VEC = RAGGED ? 4 : LANE;
+  static_assert(VEC == 4 || !BUF, "narrow rows take plain loads");
+  const StreamArgs &a = pa.s;
+  constexpr int GPB = kBlock / LPT;
+  const int lane = threadIdx.x % LPT;
+  const int grp = threadIdx.x / LPT;
+  const int c0 = blockIdx.y * (LPT * VEC) + lane * VEC;
+  const bool active = c0 < a.b;
+  const int c = lane_cols<RAGGED>(c0, a.b).c;
+  const size_t bb = (size_t)a.b;
+  const int cl = active ? c : 0;
+  // Where the lane's codes are in a row of them: its dword, or its byte.
+  const int kl = active ? c0 : 0;
+  const size_t pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
+  const uint32_t row_bytes = (uint32_t)a.b * (uint32_t)sizeof(float);
+  const uint32_t col_bytes = (uint32_t)cl * (uint32_t)sizeof(float);
+  auto rsrc = [](const void *p, uint64_t bytes, int stride) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)stride,
+                                             (int)(uint32_t)bytes, kRawBufferWord3);
+  };
+  const __amdgpu_buffer_rsrc_t arsrc = rsrc(a.A, (uint64_t)a.A_rows, (int)row_bytes);
+  const __amdgpu_buffer_rsrc_t brsrc = rsrc(pa.codes, (uint64_t)a.B_rows * pitch, 0);
+  const __amdgpu_buffer_rsrc_t orsrc = rsrc(a.out, (uint64_t)a.out_rows * row_bytes, 0);
+  const __amdgpu_buffer_rsrc_t srsrc =
+      rsrc(a.slots, (uint64_t)a.n_slots * a.b * sizeof(double), 0);
+
+  const int nl = a.n_lists;
+  const int xl = (int)(blockIdx.x % (unsigned)nl);
+  int64_t c_begin = 0, c_end = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxChunkLists; ++i)
+    if (i == xl) {
+      c_begin = a.list_chunk[i];
+      c_end = a.list_chunk[i + 1];
+    }
+  const int64_t wgs_in_list = ((int64_t)gridDim.x - xl + nl - 1) / nl;
+  const int64_t stride = wgs_in_list * GPB;
+
+  constexpr int K = (kUnroll + LPT - 1) / LPT;
+  auto fetch = [&](int64_t p, int2 (&mine)[K], float (&wmine)[K]) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t q = min(p + min(lane + k * LPT, kUnroll - 1), a.n - 1);
+      mine[k] = a.entries[q];
+      if constexpr (WEIGHTED) wmine[k] = a.weights[q];
+    }
+  };
+
+  for (int64_t g = c_begin + (blockIdx.x / nl) * GPB + grp; g < c_end; g += stride) {
+    const int64_t p0 = KBF_CHECKED(g, a.n / a.chunk) * a.chunk;
+    const int64_t p1 = p0 + a.chunk;
+    double acc[VEC];
+    float held_b[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      acc[v] = 0.0;
+      held_b[v] = 0.0f;
+    }
+    int2 mine[K];
+    float wmine[K];
+    fetch(p0, mine, wmine);
+    for (int64_t p = p0; p < p1; p += kUnroll) {
+      int2 e[kUnroll];
+      float w[kUnroll];
+      float xa[kUnroll][VEC];
+      uint32_t xb[kUnroll];
+      int exps[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const bool start = mine[k].x >= 0 && (mine[k].x & kRunStart);
+        exps[k] = pa.exponents[start ? KBF_CHECKED(mine[k].y & kIdMask, a.B_rows) : 0];
+      }
+      static_for<kUnroll>([&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+        const int2 m = mine[u / LPT];
+        e[u] = make_int2(group_bcast<LPT, u % LPT>(m.x), group_bcast<LPT, u % LPT>(m.y));
+        if constexpr (WEIGHTED)
+          w[u] = __int_as_float(group_bcast<LPT, u % LPT>(__float_as_int(wmine[u / LPT])));
+      });
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const bool triple = e[u].x >= 0;
+        const bool run_start = triple && (e[u].x & kRunStart);
+        const bool same_a = u > 0 && triple && (e[u].y & kSameA);
+        const int32_t ia = e[u].x & kIdMask, ib = e[u].y & kIdMask;
+        if constexpr (BUF) {
+          gather_row(arsrc, triple && !same_a ? (uint32_t)KBF_CHECKED(ia, a.A_rows) : kNoRecord,
+                     col_bytes, xa[u]);
+          xb[u] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(
+              brsrc,
+              (int)(run_start ? (uint32_t)KBF_CHECKED(ib, a.B_rows) * (uint32_t)pitch + (uint32_t)kl
+                              : kOutOfRange),
+              0, 0);
+        } else {
+          load_row<VEC>(a.A + (size_t)(triple ? KBF_CHECKED(ia, a.A_rows) : 0) * bb + cl, xa[u]);
+          const uint8_t *row =
+              pa.codes + (size_t)(run_start ? KBF_CHECKED(ib, a.B_rows) : 0) * pitch + kl;
+          if constexpr (VEC == 4)
+            xb[u] = *reinterpret_cast<const uint32_t *>(row);
+          else
+            xb[u] = *row;
+        }
+      }
+      int e_mine[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) e_mine[k] = exps[k] - kPackBias;
+      fetch(p + kUnroll, mine, wmine);
+      static_for<kUnroll>([&](auto uc) {
+        constexpr int u = decltype(uc)::value;
+        const bool triple = e[u].x >= 0;
+        const bool run_start = triple && (e[u].x & kRunStart);
+        if constexpr (BUF) {
+          if constexpr (u > 0) {
+            const bool same_a = triple && (e[u].y & kSameA);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) xa[u][v] = same_a ? xa[u - 1][v] : xa[u][v];
+          }
+        }
+        const int eb = group_bcast<LPT, u % LPT>(e_mine[u / LPT]);
+        float nb[VEC];
+        if constexpr (VEC == 4)
+          decode4(xb[u], eb, nb);
+        else
+          nb[0] = decode1(xb[u], eb);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          held_b[v] = run_start ? nb[v] : triple ? held_b[v] : 0.0f;
+          double t = (double)xa[u][v];
+          if constexpr (WEIGHTED) t *= (double)w[u];
+          if constexpr (!BUF) t = triple ? t : 0.0;
+          acc[v] = __builtin_fma(t, (double)held_b[v], acc[v]);
+        }
+        const int f = e[u].y;
+        if (!triple) {
+          if (active && f != INT_MIN) {
+            if (f >= 0) {
+              if constexpr (BUF)
+                store_row_buffer(orsrc,
+                                 (uint32_t)KBF_CHECKED(f, a.out_rows) * row_bytes + col_bytes, acc);
+              else
+                store_row<VEC>(a.out + (size_t)KBF_CHECKED(f, a.out_rows) * bb + c, acc);
+            } else {
+              if constexpr (BUF)
+                store_slot_buffer(
+                    srsrc,
+                    ((uint32_t)KBF_CHECKED(-(f + 1), a.n_slots) * (uint32_t)a.b + (uint32_t)c) *
+                        (uint32_t)sizeof(double),
+                    acc);
+              else
+                store_slot<VEC>(a.slots + (size_t)KBF_CHECKED(-(f + 1), a.n_slots) * bb + c, acc);
+            }
+          }
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) acc[v] = 0.0;
+        }
+      });
+    }
+  }
+}
+
+// The exponent byte of a row whose largest finite size has the bits `top`:
+// 448 = 1.75 * 2^8, so from the exponent 8 less, 7 where the mantissa passes 1.75.
+__device__ __forceinline__ int pack_exponent(uint32_t top) {
+  return max(0, (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u));
+}
+__device__ __forceinline__ uint32_t size_bits(float x) {
+  const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
+  return u < 0x7F800000u ? u : 0;  // infinities and NaN set no exponent
+}
+constexpr uint32_t kPackNaN = 0x7F;
+// The code of x / 2^e (e4m3 has no infinities: they are kept as NaN, as NaN is).
+// Under the largest exponent, 120, the code of 240 is the last whose value is a
+// float: 256 * 2^120, to which the largest floats would round, is not.
+__device__ __forceinline__ uint32_t encode1(float x, int e) {
+  const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
+  const float most = e == 120 ? 240.0f : 448.0f;
+  const float y = fminf(fmaxf(__builtin_ldexpf(finite ? x : 0.0f, -e), -most), most);
+  const uint32_t code = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xFFu;
+  return finite ? code : kPackNaN;
+}
+
+// A lane group of LPT lanes per row, kPackRows rows of it in flight; rows of
+// more than LPT vectors take a second look at what they read.  Bound by the bytes
+// moved: a float read, a byte written (and the other way round).
+constexpr int kPackRows = 4;
+
+template <int VEC, int LPT>
+__global__ __launch_bounds__(kBlock) void pack_kernel(const float *__restrict__ X, int64_t rows,
+                                                      int32_t b, uint8_t *__restrict__ codes,
+                                                      uint8_t *__restrict__ exponents) {
+  constexpr int GPB = kBlock / LPT;
+  const int lane = threadIdx.x % LPT;
+  const int64_t r0 = ((int64_t)blockIdx.x * GPB + threadIdx.x / LPT) * kPackRows;
+  const size_t bb = (size_t)b, pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
+  auto col = [&](int c0) { return VEC == 4 ? min(c0, b - 4) : c0; };
+  float x[kPackRows][VEC];
+  uint32_t top[kPackRows];
+#pragma unroll
+  for (int k = 0; k < kPackRows; ++k) {
+    const int64_t r = min(r0 + k, rows - 1);
+    top[k] = 0;
+    if (lane * VEC < b) {
+      load_row<VEC>(X + (size_t)r * bb + col(lane * VEC), x[k]);
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) x[k][v] = 0.0f;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kPackRows; ++k) {
+    const int64_t r = min(r0 + k, rows - 1);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) top[k] = max(top[k], size_bits(x[k][v]));
+    for (int64_t c0 = (int64_t)(lane + LPT) * VEC; c0 < b; c0 += LPT * VEC) {
+      float y[VEC];
+      load_row<VEC>(X + (size_t)r * bb + col((int)c0), y);
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) top[k] = max(top[k], size_bits(y[v]));
+    }
+#pragma unroll
+    for (int m = 1; m < LPT; m <<= 1) top[k] = max(top[k], (uint32_t)__shfl_xor((int)top[k], m));
+  }
+#pragma unroll
+  for (int k = 0; k < kPackRows; ++k) {
+    const int64_t r = r0 + k;
+    if (r >= rows) break;
+    const int byte = pack_exponent(top[k]), e = byte - kPackBias;
+    if (lane == 0) exponents[r] = (uint8_t)byte;
+    auto put = [&](int c0, const float (&y)[VEC]) {
+      uint8_t *at = codes + (size_t)r * pitch + c0;
+      if constexpr (VEC == 4)
+        *reinterpret_cast<uint32_t *>(at) = encode1(y[0], e) | encode1(y[1], e) << 8 |
+                                            encode1(y[2], e) << 16 | encode1(y[3], e) << 24;
+      else
+        *at = (uint8_t)encode1(y[0], e);
+    };
+    if (lane * VEC < b) put(lane * VEC, x[k]);
+    for (int64_t c0 = (int64_t)(lane + LPT) * VEC; c0 < b; c0 += LPT * VEC) {
+      float y[VEC];
+      load_row<VEC>(X + (size_t)r * bb + col((int)c0), y);
+      put((int)c0, y);
+    }
+  }
+}
+
+template <int VEC, int LPT>
+__global__ __launch_bounds__(kBlock) void unpack_kernel(const uint8_t *__restrict__ codes,
+                                                        const uint8_t *__restrict__ exponents,
+                                                        int64_t rows, int32_t b,
+                                                        float *__restrict__ X) {
+  constexpr int GPB = kBlock / LPT;
+  const int lane = threadIdx.x % LPT;
+  const int64_t r0 = ((int64_t)blockIdx.x * GPB + threadIdx.x / LPT) * kPackRows;
+  const size_t bb = (size_t)b, pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
+  int e[kPackRows];
+#pragma unroll
+  for (int k = 0; k < kPackRows; ++k) e[k] = (int)exponents[min(r0 + k, rows - 1)] - kPackBias;
+  for (int64_t c0 = (int64_t)lane * VEC; c0 < b; c0 += LPT * VEC) {
+    uint32_t x[kPackRows];
+#pragma unroll
+    for (int k = 0; k < kPackRows; ++k) {
+      const uint8_t *at = codes + (size_t)min(r0 + k, rows - 1) * pitch + c0;
+      if constexpr (VEC == 4)
+        x[k] = *reinterpret_cast<const uint32_t *>(at);
+      else
+        x[k] = *at;
+    }
+#pragma unroll
+    for (int k = 0; k < kPackRows; ++k) {
+      if (r0 + k >= rows) break;
+      float *to = X + (size_t)(r0 + k) * bb + (VEC == 4 ? min((int)c0, b - 4) : (int)c0);
+      if constexpr (VEC == 4) {
+        float v[4];
+        decode4(x[k], e[k], v);
+        const double d[4] = {v[0], v[1], v[2], v[3]};
+        store_row<4>(to, d);
+      } else {
+        *to = decode1(x[k], e[k]);
+      }
+    }
+  }
+}
+
 // Adds slots [first, first + n) in increasing order; writes the float row or
 // a next-level slot.  `block` of `n_blocks` blocks share the tasks.
 template <int VEC, int LPT, bool RAGGED>
@@ -1366,6 +1678,131 @@ hipError_t launch_stream(const StreamArgs &a, const StreamOptions &o, hipStream_
   if (start || stop)
     return hipExtLaunchKernel(c.fn, c.grid, dim3(c.block), params, c.lds_bytes, s, start, stop, 0);
   return hipLaunchKernel(c.fn, c.grid, dim3(c.block), params, c.lds_bytes, s);
+}
+
+namespace {
+
+template <int LANE, bool BUF, bool WT>
+const void *packed_fn(int lpt) {
+  switch (lpt) {
+    case 1:
+      if constexpr (LANE == kRaggedLane)
+        return nullptr;
+      else
+        return reinterpret_cast<const void *>(&packed_kernel<LANE, 1, BUF, WT>);
+    case 2:
+      return reinterpret_cast<const void *>(&packed_kernel<LANE, 2, BUF, WT>);
+    case 4:
+      return reinterpret_cast<const void *>(&packed_kernel<LANE, 4, BUF, WT>);
+  }
+  if constexpr (LANE != 1) {
+    switch (lpt) {
+      case 8: return reinterpret_cast<const void *>(&packed_kernel<LANE, 8, BUF, WT>);
+      case 16: return reinterpret_cast<const void *>(&packed_kernel<LANE, 16, BUF, WT>);
+      case 32: return reinterpret_cast<const void *>(&packed_kernel<LANE, 32, BUF, WT>);
+    }
+  }
+  return nullptr;
+}
+
+const void *packed_fn_for(const ColumnTiling &t, bool buf, bool wt) {
+  if (t.vec == 1) return wt ? packed_fn<1, false, true>(t.lpt) : packed_fn<1, false, false>(t.lpt);
+  if (t.ragged) {
+    if (buf)
+      return wt ? packed_fn<kRaggedLane, true, true>(t.lpt)
+                : packed_fn<kRaggedLane, true, false>(t.lpt);
+    return wt ? packed_fn<kRaggedLane, false, true>(t.lpt)
+              : packed_fn<kRaggedLane, false, false>(t.lpt);
+  }
+  if (buf) return wt ? packed_fn<4, true, true>(t.lpt) : packed_fn<4, true, false>(t.lpt);
+  return wt ? packed_fn<4, false, true>(t.lpt) : packed_fn<4, false, false>(t.lpt);
+}
+
+// f(vec, lanes) for rows of b floats, as constants.
+template <class F>
+hipError_t with_pack_lanes(int32_t b, F f) {
+  const int lanes = b < 4 ? b : (b + 3) / 4;
+  int lpt = 1;
+  while (lpt < lanes && lpt < 64) lpt <<= 1;
+  if (b < 4) {
+    if (lpt == 1) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
+    if (lpt == 2) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
+    return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+  }
+  constexpr std::integral_constant<int, 4> four{};
+  switch (lpt) {
+    case 1: return f(four, std::integral_constant<int, 1>{});
+    case 2: return f(four, std::integral_constant<int, 2>{});
+    case 4: return f(four, std::integral_constant<int, 4>{});
+    case 8: return f(four, std::integral_constant<int, 8>{});
+    case 16: return f(four, std::integral_constant<int, 16>{});
+    case 32: return f(four, std::integral_constant<int, 32>{});
+    default: return f(four, std::integral_constant<int, 64>{});
+  }
+}
+
+}  // namespace
+
+hipError_t launch_packed(const PackedArgs &p, const StreamOptions &o, hipStream_t s,
+                         hipEvent_t start, hipEvent_t stop) {
+  const StreamArgs &a = p.s;
+  if (a.n == 0) return hipSuccess;
+  if (a.chunk % kChunkQuantum != 0 || a.n % a.chunk != 0 || a.residual || a.n_lists < 1 ||
+      a.n_lists > kMaxChunkLists || a.list_chunk[0] != 0 ||
+      a.list_chunk[a.n_lists] != a.n / a.chunk)
+    return hipErrorInvalidValue;
+  int64_t longest = 0;
+  for (int x = 0; x < a.n_lists; ++x) {
+    if (a.list_chunk[x + 1] < a.list_chunk[x]) return hipErrorInvalidValue;
+    longest = std::max<int64_t>(longest, a.list_chunk[x + 1] - a.list_chunk[x]);
+  }
+  const ColumnTiling t = column_tiling_max(a.b, std::max(1, std::min(o.max_lpt, kMaxLpt)));
+  const uint64_t row_bytes = (uint64_t)a.b * sizeof(float), lim = kOutOfRange;
+  const bool buf = !o.plain_loads && t.vec == 4 && row_bytes <= kMaxStride &&
+                   (uint64_t)a.A_rows * row_bytes <= lim &&
+                   (uint64_t)a.B_rows * (uint64_t)packed_pitch(a.b) <= lim &&
+                   (uint64_t)a.out_rows * row_bytes <= lim &&
+                   (uint64_t)a.n_slots * (uint64_t)a.b * sizeof(double) <= lim;
+  // Groups of at least two lanes for ragged rows, which are of 5 floats or more.
+  ColumnTiling u = t;
+  if (u.ragged && u.lpt < 2) u.lpt = 2;
+  u.width = u.lpt * u.vec;
+  u.n_slices = (a.b + u.width - 1) / u.width;
+  const void *fn = packed_fn_for(u, buf, a.weights != nullptr);
+  if (!fn) return hipErrorInvalidValue;
+  const int64_t per_list =
+      std::max<int64_t>(1, (longest + kBlock / u.lpt - 1) / (kBlock / u.lpt));
+  if (per_list * a.n_lists > (int64_t)INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(per_list * a.n_lists), (unsigned)u.n_slices);
+  PackedArgs arg = p;
+  void *params[] = {&arg};
+  if (start || stop)
+    return hipExtLaunchKernel(fn, grid, dim3(kBlock), params, 0, s, start, stop, 0);
+  return hipLaunchKernel(fn, grid, dim3(kBlock), params, 0, s);
+}
+
+hipError_t launch_pack(const float *X, int64_t rows, int32_t b, uint8_t *codes,
+                       uint8_t *exponents, hipStream_t s) {
+  return with_pack_lanes(b, [&](auto vec, auto lanes) {
+    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
+    const int64_t per = (int64_t)kBlock / L * kPackRows, blocks = (rows + per - 1) / per;
+    if (blocks * kBlock > (int64_t)UINT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((pack_kernel<V, L>), dim3((unsigned)blocks), dim3(kBlock), 0, s, X, rows, b,
+                       codes, exponents);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_unpack(const uint8_t *codes, const uint8_t *exponents, int64_t rows, int32_t b,
+                         float *X, hipStream_t s) {
+  return with_pack_lanes(b, [&](auto vec, auto lanes) {
+    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
+    const int64_t per = (int64_t)kBlock / L * kPackRows, blocks = (rows + per - 1) / per;
+    if (blocks * kBlock > (int64_t)UINT32_MAX) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((unpack_kernel<V, L>), dim3((unsigned)blocks), dim3(kBlock), 0, s, codes,
+                       exponents, rows, b, X);
+    return hipGetLastError();
+  });
 }
 
 std::string describe_stream(const StreamArgs &a, const StreamOptions &o) {
