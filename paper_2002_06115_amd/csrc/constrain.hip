@@ -40,7 +40,7 @@ enum Allowed { kAll, kBytes, kBits };
 struct Args {
   int64_t n;
   int32_t b;
-  uint32_t magic;  // ceil(2^32 / b), for b <= kTile
+  uint32_t magic;  // ceil(2^32 / b), for b <= kMostTile
   const void *z;   // logits (forward), or null
   const float *dout;
   const float *bias;
@@ -65,22 +65,25 @@ __device__ __forceinline__ float bias_of(const Args &a, int64_t i, int32_t col) 
 
 // -- every element, as if no history were ---------------------------------------------
 
-constexpr int kDepth = 4;                      // vectors of 4 elements of a thread
-constexpr int kTile = kThreads * 4 * kDepth;   // elements of a workgroup
+// Vectors of 4 elements of a thread, and elements of a workgroup: DEPTH 1 where an
+// array is small and latency counts, 4 where it is large.
+template <int DEPTH>
+constexpr int kTile = kThreads * 4 * DEPTH;
+constexpr int kMostTile = kTile<4>;
 
 // BACKWARD: dz (and a bias' own gradient, one an element) from dout.
-template <class T, bool BACKWARD>
+template <class T, bool BACKWARD, int DEPTH>
 __global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
   using In = std::conditional_t<BACKWARD, float, T>;
   using Out = std::conditional_t<BACKWARD, T, float>;
   const In *in = BACKWARD ? reinterpret_cast<const In *>(a.dout) : static_cast<const In *>(a.z);
   Out *out = static_cast<Out *>(a.out);
-  const int64_t first = (int64_t)blockIdx.x * kTile, size = a.n * a.b;
+  const int64_t first = (int64_t)blockIdx.x * kTile<DEPTH>, size = a.n * a.b;
   const int64_t row0 = first / a.b;
   const uint32_t rest = (uint32_t)(first - row0 * a.b);
-  vec4_any<In> v[kDepth];
+  vec4_any<In> v[DEPTH];
 #pragma unroll
-  for (int k = 0; k < kDepth; ++k) {
+  for (int k = 0; k < DEPTH; ++k) {
     const int64_t f = first + (k * kThreads + (int)threadIdx.x) * 4;
     if (f + 4 <= size) {
       v[k] = *reinterpret_cast<const vec4_any<In> *>(in + f);
@@ -90,14 +93,14 @@ __global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
     }
   }
 #pragma unroll
-  for (int k = 0; k < kDepth; ++k) {
+  for (int k = 0; k < DEPTH; ++k) {
     const uint32_t local = (uint32_t)(k * kThreads + (int)threadIdx.x) * 4;
     const int64_t f = first + local;
     if (f >= size) break;
     // The row and column of the first of the four: exact, as the dividend is
-    // below 2 b where b is above kTile, and below 2 kTile where it is not.
+    // below 2 b where b is above kMostTile, and below 2 kMostTile where it is not.
     const uint32_t x = rest + local;
-    const uint32_t q = a.b > kTile ? (uint32_t)(x >= (uint32_t)a.b) : a.b == 1 ? x : __umulhi(x, a.magic);
+    const uint32_t q = a.b > kMostTile ? (uint32_t)(x >= (uint32_t)a.b) : a.b == 1 ? x : __umulhi(x, a.magic);
     int64_t i = row0 + q;
     int32_t col = (int32_t)(x - q * (uint32_t)a.b);
     float y[4];
@@ -185,9 +188,18 @@ struct Penalties {
   float repeat_all, presence_all, frequency_all;
 };
 
-constexpr int kEntryLanes = 8;                       // lanes that share an entry's count
+// Lanes that share an entry's count: 15200 ids of 8 columns take 14 us with 16 lanes,
+// 17 with 8, 27 with 4.
+constexpr int kEntryLanes = 16;
 constexpr int kEntries = kThreads / kEntryLanes;     // entries of a workgroup
 constexpr int kBlockIds = 2048;                      // ids in LDS at a time
+constexpr int kCompare = 4;                          // quads of them in flight
+
+// The row that entry t names, -1 for padding.
+__device__ __forceinline__ int row_of(const Penalties &p, int64_t n, int64_t t) {
+  const int64_t id = load_int(p.ids, t);
+  return id >= 0 && id < n ? (int)id : -1;
+}
 
 template <class T, bool BACKWARD>
 __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) {
@@ -197,11 +209,11 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
   const int lane = threadIdx.x % kEntryLanes;
   const int64_t t0 = (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / kEntryLanes;
   const int64_t total = p.columns.tokens;
-  const int64_t col = t < total ? bag_of(p.columns, t) : -1;
-  int64_t id = -1, begin = 0, end = 0;
+  const int64_t col = t < total ? bag_of_lanes<kEntryLanes>(p.columns, t, lane) : -1;
+  int id = -1;
+  int64_t begin = t, end = t + 1;  // the ids of the entry's column
   if (col >= 0) {
-    id = load_int(p.ids, t);
-    if (id >= a.n) id = -1;
+    id = row_of(p, a.n, t);
     begin = bag_begin(p.columns, col);
     end = bag_begin(p.columns, col + 1);
   }
@@ -210,42 +222,52 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
   int count = 0;
   if (counts) {  // uniform
     // The ids of every column that the workgroup's entries are of.
-    if (threadIdx.x == 0) {
-      const int64_t c0 = bag_of(p.columns, t0);
-      const int64_t c1 = bag_of(p.columns, min(t0 + kEntries, total) - 1);
-      range[0] = c0 < 0 ? t0 : bag_begin(p.columns, c0);
-      range[1] = c1 < 0 ? t0 + kEntries : bag_begin(p.columns, c1 + 1);
-    }
+    if (threadIdx.x == 0) range[0] = begin;
+    if (lane == 0 && t == min(t0 + kEntries, total) - 1) range[1] = end;
     __syncthreads();
     const int64_t r1 = min(range[1], total);
+    // The next block is on its way while one is compared.
+    int next[kBlockIds / kThreads];
+    auto fetch = [&](int64_t r0) {
+#pragma unroll
+      for (int u = 0; u < kBlockIds / kThreads; ++u)
+        next[u] = row_of(p, a.n, min(r0 + u * kThreads + threadIdx.x, r1 - 1));
+    };
+    if (range[0] < r1) fetch(range[0]);
     for (int64_t r0 = range[0]; r0 < r1; r0 += kBlockIds) {
       __syncthreads();  // the block before has been read
-      for (int k = threadIdx.x; k < kBlockIds; k += kThreads) {
-        const int64_t x = r0 + k < r1 ? load_int(p.ids, r0 + k) : -1;
-        ids[k] = x >= 0 && x < a.n ? (int)x : -1;
-      }
+#pragma unroll
+      for (int u = 0; u < kBlockIds / kThreads; ++u) ids[u * kThreads + threadIdx.x] = next[u];
       __syncthreads();
+      if (r0 + kBlockIds < r1) fetch(r0 + kBlockIds);
       if (valid) {
         const int lo = (int)max((int64_t)0, begin - r0);
         const int hi = (int)min((int64_t)kBlockIds, end - r0);
-        for (int q = lo / 4 + lane; q * 4 < hi; q += kEntryLanes) {
-          const int4 x = lds[q];
-          if (q * 4 >= lo && q * 4 + 4 <= hi) {
-            count += (x.x == id) + (x.y == id) + (x.z == id) + (x.w == id);
-          } else {
-            const int at = q * 4;
-            count += (x.x == id && at >= lo && at < hi) + (x.y == id && at + 1 >= lo && at + 1 < hi) +
-                     (x.z == id && at + 2 >= lo && at + 2 < hi) +
-                     (x.w == id && at + 3 >= lo && at + 3 < hi);
-          }
+        // Whole quads of the column, kCompare in flight, then its ends one by one.
+        const int q0 = (lo + 3) / 4, q1 = hi / 4;
+        int q = q0 + lane;
+        for (; q + (kCompare - 1) * kEntryLanes < q1; q += kCompare * kEntryLanes) {
+          int4 x[kCompare];
+#pragma unroll
+          for (int u = 0; u < kCompare; ++u) x[u] = lds[q + u * kEntryLanes];
+#pragma unroll
+          for (int u = 0; u < kCompare; ++u)
+            count += (x[u].x == id) + (x[u].y == id) + (x[u].z == id) + (x[u].w == id);
         }
+        for (; q < q1; q += kEntryLanes) {
+          const int4 x = lds[q];
+          count += (x.x == id) + (x.y == id) + (x.z == id) + (x.w == id);
+        }
+        const int head = lo + lane, tail = max(q1, q0) * 4 + lane;
+        if (head < min(q0 * 4, hi)) count += ids[head] == id;
+        if (tail < hi) count += ids[tail] == id;
       }
     }
 #pragma unroll
     for (int m = 1; m < kEntryLanes; m <<= 1) count += __shfl_xor(count, m);
   }
   if (!valid || lane != 0) return;
-  const int64_t f = id * a.b + col;
+  const int64_t f = (int64_t)id * a.b + col;
   const bool ok = is_allowed(a, id, (int32_t)col);
   const double repeat = p.repeat ? p.repeat[col] : p.repeat_all;
   const double z = (double)(float)static_cast<const T *>(a.z)[f];
@@ -263,6 +285,11 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
 
 // -- how a call is launched ----------------------------------------------------------------
 
+// Elements from which workgroups take 4 vectors a thread: 4 million of 43000 rows
+// of 93 columns take 13.2 us with one vector and 14.5 with four (with the history's
+// launch), 64 million 92 to 100 and 97 to 100.
+constexpr int64_t kSmall = 1 << 22;
+
 template <class F>
 void with_type(kbc_type type, F f) {
   switch (type) {
@@ -274,7 +301,7 @@ void with_type(kbc_type type, F f) {
 
 bool bad_limits(int64_t n, int32_t b, kbc_type type, const kbc_limits *l) {
   if (n < 1 || n > kMostRows || b < 1 || bad_type(type) || !l) return true;
-  if (ceil_div(n * b, kTile) > kMostBlocks || ceil_div(n, 4) > kMostBlocks) return true;
+  if (ceil_div(n * b, kMostTile) > kMostBlocks || ceil_div(n, 4) > kMostBlocks) return true;
   if (l->entries < 0 || l->entries > kMostTokens) return true;
   if (l->entries > 0) {
     if (!l->history || (l->id_bytes != 4 && l->id_bytes != 8)) return true;
@@ -302,6 +329,17 @@ Penalties penalties_for(int32_t b, const kbc_limits *l) {
           l->repeat, l->presence, l->frequency, l->repeat_all, l->presence_all, l->frequency_all};
 }
 
+template <class T, bool BACKWARD>
+void launch_dense(const Args &a, hipStream_t s) {
+  const int64_t size = a.n * a.b;
+  if (size < kSmall)
+    hipLaunchKernelGGL((dense_kernel<T, BACKWARD, 1>), dim3((unsigned)ceil_div(size, kTile<1>)),
+                       dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((dense_kernel<T, BACKWARD, 4>), dim3((unsigned)ceil_div(size, kTile<4>)),
+                       dim3(kThreads), 0, s, a);
+}
+
 template <class T, int G>
 void launch_rows(const Args &a, hipStream_t s) {
   hipLaunchKernelGGL((row_kernel<T, G>), dim3((unsigned)ceil_div(a.n, kThreads / G)),
@@ -325,8 +363,7 @@ kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, con
                                             l->frequency_all != 0.0f);
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL((dense_kernel<T, false>), dim3((unsigned)ceil_div(n * b, kTile)),
-                       dim3(kThreads), 0, s, a);
+    launch_dense<T, false>(a, s);
     if (penalised)
       hipLaunchKernelGGL((history_kernel<T, false>), dim3((unsigned)ceil_div(l->entries, kEntries)),
                          dim3(kThreads), 0, s, a, penalties_for(b, l));
@@ -362,8 +399,7 @@ kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type 
       else
         launch_rows<T, 64>(a, s);
     } else {
-      hipLaunchKernelGGL((dense_kernel<T, true>), dim3((unsigned)ceil_div(n * b, kTile)),
-                         dim3(kThreads), 0, s, a);
+      launch_dense<T, true>(a, s);
     }
     if (scaled)
       hipLaunchKernelGGL((history_kernel<T, true>), dim3((unsigned)ceil_div(l->entries, kEntries)),

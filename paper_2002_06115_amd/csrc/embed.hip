@@ -15,13 +15,14 @@
 // order; a row that lies inside its chunk is written at once, a row that crosses
 // chunks leaves one partial sum per chunk, added in order by the second launch.
 // So the work is spread evenly however often a word occurs, nothing is atomic,
-// and two calls give the same bits.  Sums are taken in double; an output is
+// and two calls give the same bits.  Sums are taken in double (see Slot); an output is
 // rounded to float and, in a 16-bit type, from there to the type.
 //
 // The list is sorted by the tokens' ids, stably.  Up to kRankTokens tokens, each
 // token's place is counted: the number of tokens with a smaller id, or the same
 // and before it, against all ids in LDS, in one launch over the whole chip.
-// More take a radix sort, up to 9 bits a pass, three launches each.
+// More take a radix sort, up to 9 bits a pass, three launches each, which also clear
+// the output by shares, as they leave the memory idle.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,21 +36,22 @@ namespace {
 
 using namespace kbc;
 
+constexpr int kWaves = kThreads / kWave;
+
 // -- rows of a type ---------------------------------------------------------------
 
-// 16 bytes of a row, wherever the row begins.
+// Neighbouring values of a row, wherever the row begins: 16 bytes of them.
+template <class T, int VEC>
+using vec_any = T __attribute__((ext_vector_type(VEC), aligned(sizeof(T))));
 template <class T>
-struct Row {
-  static constexpr int kVec = 16 / (int)sizeof(T);
-  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
-};
+constexpr int kVec = 16 / (int)sizeof(T);
 
 template <class T, int VEC>
 __device__ __forceinline__ void load_vals(const T *p, T (&v)[VEC]) {
   if constexpr (VEC == 1) {
     v[0] = *p;
   } else {
-    const typename Row<T>::vec t = *reinterpret_cast<const typename Row<T>::vec *>(p);
+    const vec_any<T, VEC> t = *reinterpret_cast<const vec_any<T, VEC> *>(p);
 #pragma unroll
     for (int k = 0; k < VEC; ++k) v[k] = t[k];
   }
@@ -61,10 +63,10 @@ __device__ __forceinline__ void store_vals(T *p, const T (&v)[VEC]) {
   if constexpr (VEC == 1) {
     *p = v[0];
   } else {
-    typename Row<T>::vec t;
+    vec_any<T, VEC> t;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) t[k] = v[k];
-    __builtin_nontemporal_store(t, reinterpret_cast<typename Row<T>::vec *>(p));
+    __builtin_nontemporal_store(t, reinterpret_cast<vec_any<T, VEC> *>(p));
   }
 }
 
@@ -194,8 +196,9 @@ struct ListArgs {
   void *fill;       // output rows to clear, in words of 4 bytes and a rest of 2
   int64_t fill_bytes;
   int2 *entries;
-  // workgroups of the launch: list_wgs make the list, then weight_wgs, then the fill's
-  uint32_t list_wgs, weight_wgs;
+  // workgroups of a launch: list_wgs make the list, then weight_wgs, then those of a
+  // share of the fill, from its piece first_fill on
+  uint32_t list_wgs, weight_wgs, first_fill;
 };
 
 // Token t's key in the gradient's list: its id, or `rows` where it names none.
@@ -221,10 +224,10 @@ __device__ __forceinline__ int count_ids(const ListArgs &a, int64_t begin, int64
   return n;
 }
 __device__ void bag_weights(const ListArgs &a, int64_t block) {
-  __shared__ int counts[kThreads / kWave];
+  __shared__ int counts[kWaves];
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  for (int k = 0; k < kThreads / kWave; ++k) {
-    const int64_t g = block * (kThreads / kWave) + k;
+  for (int k = 0; k < kWaves; ++k) {
+    const int64_t g = block * kWaves + k;
     if (g >= a.bags.n) break;
     const int64_t begin = bag_begin(a.bags, g), end = bag_begin(a.bags, g + 1);
     if (end - begin < kLongBag) {  // the same for the whole workgroup
@@ -238,7 +241,7 @@ __device__ void bag_weights(const ListArgs &a, int64_t block) {
       __syncthreads();
       if (threadIdx.x == 0) {
         int all = 0;
-        for (int w = 0; w < kThreads / kWave; ++w) all += counts[w];
+        for (int w = 0; w < kWaves; ++w) all += counts[w];
         a.weights[g] = all > 0 ? 1.0 / (double)all : 0.0;
       }
     }
@@ -261,14 +264,14 @@ __device__ __forceinline__ void clear(const ListArgs &a, int64_t block) {
   }
 }
 
-// What the workgroups past list_wgs of a list's first launch do.
+// What the workgroups past list_wgs of a launch do.
 __device__ __forceinline__ bool other_work(const ListArgs &a) {
   if (blockIdx.x < a.list_wgs) return false;
   const uint32_t k = blockIdx.x - a.list_wgs;
   if (k < a.weight_wgs)
     bag_weights(a, k);
   else
-    clear(a, k - a.weight_wgs);
+    clear(a, (int64_t)a.first_fill + (k - a.weight_wgs));
   return true;
 }
 
@@ -285,8 +288,11 @@ __global__ __launch_bounds__(kThreads) void pool_list_kernel(ListArgs a) {
 
 // -- the gradient's list, few tokens: places counted ----------------------------------
 
+// (16389 tokens: gradient 111 us counted, 94 sorted.)
 constexpr int64_t kRankTokens = 8192;
 constexpr int kRankLanes = 8;                          // lanes that share a token's count
+constexpr int kRankDepth = 4;                          // quads of keys in flight
+constexpr int kRankLoads = 8;                          // ids in flight on their way to LDS
 constexpr int kRankPer = kThreads / kRankLanes;        // tokens of a workgroup
 
 __global__ __launch_bounds__(kThreads) void rank_kernel(ListArgs a) {
@@ -294,31 +300,63 @@ __global__ __launch_bounds__(kThreads) void rank_kernel(ListArgs a) {
   extern __shared__ int4 rank_lds[];
   int *keys = reinterpret_cast<int *>(rank_lds);
   const int n = (int)a.tokens, quads = (n + 3) / 4;
-  for (int t = threadIdx.x; t < quads * 4; t += kThreads)
-    keys[t] = t < n ? key_of(a, t) : INT32_MAX;
-  __syncthreads();
+  for (int t0 = threadIdx.x; t0 < quads * 4; t0 += kThreads * kRankLoads) {
+    int k[kRankLoads];
+#pragma unroll
+    for (int u = 0; u < kRankLoads; ++u) k[u] = key_of(a, min(t0 + u * kThreads, n - 1));
+#pragma unroll
+    for (int u = 0; u < kRankLoads; ++u) {
+      const int t = t0 + u * kThreads;
+      if (t < quads * 4) keys[t] = t < n ? k[u] : INT32_MAX;
+    }
+  }
   const int lane = threadIdx.x % kRankLanes;
   const int t = blockIdx.x * kRankPer + threadIdx.x / kRankLanes;
+  // Searched for while the keys are on their way.
+  const int src = a.bags.n ? (int)bag_of_lanes<kRankLanes>(a.bags, min(t, n - 1), lane) : t;
+  __syncthreads();
   const int key = keys[min(t, n - 1)];
-  // Four keys at a time; those of t's own four are told apart one by one.
+  // Four keys at a time, kRankDepth times: all up to the token's own four count that
+  // are not larger, all behind that are smaller; those four one by one.
   int place = 0;
   const int own = t / 4;
-  for (int q = lane; q < quads; q += kRankLanes) {
-    const int4 k = rank_lds[q];
-    const int bar = q < own ? key : key - 1;  // (keys are not negative)
-    place += (k.x <= bar) + (k.y <= bar) + (k.z <= bar) + (k.w <= bar);
-  }
+  auto count = [&](int from, int to, int bar) {
+    int q = from + lane;
+    for (; q + (kRankDepth - 1) * kRankLanes < to; q += kRankDepth * kRankLanes) {
+      int4 k[kRankDepth];
+#pragma unroll
+      for (int u = 0; u < kRankDepth; ++u) k[u] = rank_lds[q + u * kRankLanes];
+#pragma unroll
+      for (int u = 0; u < kRankDepth; ++u)
+        place += (k[u].x <= bar) + (k[u].y <= bar) + (k[u].z <= bar) + (k[u].w <= bar);
+    }
+    for (; q < to; q += kRankLanes) {
+      const int4 k = rank_lds[q];
+      place += (k.x <= bar) + (k.y <= bar) + (k.z <= bar) + (k.w <= bar);
+    }
+  };
+  count(0, min(own, quads), key);
+  count(own, quads, key - 1);  // (keys are not negative)
   if (lane == own % kRankLanes)
     for (int j = own * 4; j < t && j < n; ++j) place += keys[j] == key;
 #pragma unroll
   for (int m = 1; m < kRankLanes; m <<= 1) place += __shfl_xor(place, m);
-  if (lane == 0 && t < n) a.entries[place] = grad_entry(a, key, t);
+  if (lane == 0 && t < n) a.entries[place] = make_int2(key, src);
 }
 
 // -- the gradient's list, many tokens: radix sort -------------------------------------
 
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
-constexpr int kTileItems = 8, kTile = kThreads * kTileItems;
+// Entries of a thread: 2, which keeps a workgroup's steps few (262144 tokens on 512
+// workgroups 142 us for the whole gradient, with 8 on 128 154; 16389 tokens 82
+// against 95); 8 for long lists, whose counts would be many.
+constexpr int64_t kLongList = 1 << 20;
+template <int ITEMS>
+constexpr int kTile = kThreads * ITEMS;
+int64_t tiles_of(int64_t tokens) {
+  const int64_t tile = tokens < kLongList ? kTile<2> : kTile<8>;
+  return (tokens + tile - 1) / tile;
+}
 
 struct RadixArgs {
   ListArgs list;
@@ -334,15 +372,16 @@ __device__ __forceinline__ int radix_key(const RadixArgs &a, int64_t i) {
   return a.in ? a.in[i].x : key_of(a.list, i);
 }
 
+template <int ITEMS>
 __global__ __launch_bounds__(kThreads) void radix_count_kernel(RadixArgs a) {
   if (other_work(a.list)) return;
   __shared__ uint32_t count[kDigits];
   const int digits = 1 << a.bits;
   for (int i = threadIdx.x; i < digits; i += kThreads) count[i] = 0;
   __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kTile;
+  const int64_t base = (int64_t)blockIdx.x * kTile<ITEMS>;
 #pragma unroll
-  for (int k = 0; k < kTileItems; ++k) {
+  for (int k = 0; k < ITEMS; ++k) {
     const int64_t i = base + k * kThreads + threadIdx.x;
     if (i < a.list.tokens) atomicAdd(&count[(radix_key(a, i) >> a.shift) & (digits - 1)], 1u);
   }
@@ -365,7 +404,7 @@ __device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *lds, uint
   __syncthreads();
   uint32_t before = 0, sum = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / kWave; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     if (w < wave) before += lds[w];
     sum += lds[w];
   }
@@ -374,58 +413,40 @@ __device__ __forceinline__ uint32_t scan_threads(uint32_t v, uint32_t *lds, uint
 }
 
 // One workgroup per digit: its counts become the entries in the tiles before.
-__global__ __launch_bounds__(kThreads) void radix_scan_kernel(uint32_t tiles, uint32_t *counts,
-                                                              uint32_t *totals) {
-  __shared__ uint32_t lds[kThreads / kWave];
-  uint32_t *c = counts + (int64_t)blockIdx.x * tiles;
+__global__ __launch_bounds__(kThreads) void radix_scan_kernel(RadixArgs a) {
+  if (other_work(a.list)) return;
+  __shared__ uint32_t lds[kWaves];
+  uint32_t *c = a.counts + (int64_t)blockIdx.x * a.tiles;
   uint32_t sum = 0;
-  for (uint32_t i0 = 0; i0 < tiles; i0 += kThreads) {
+  for (uint32_t i0 = 0; i0 < a.tiles; i0 += kThreads) {
     const uint32_t i = i0 + threadIdx.x;
-    const uint32_t v = i < tiles ? c[i] : 0;
+    const uint32_t v = i < a.tiles ? c[i] : 0;
     uint32_t all;
     const uint32_t before = scan_threads(v, lds, &all);
-    if (i < tiles) c[i] = sum + before;
+    if (i < a.tiles) c[i] = sum + before;
     sum += all;
   }
-  if (threadIdx.x == 0) totals[blockIdx.x] = sum;
+  if (threadIdx.x == 0) a.totals[blockIdx.x] = sum;
 }
 
-// Each wave places 512 consecutive entries, 64 at a time in order: lanes of one
+// Each wave places 64 ITEMS consecutive entries, 64 at a time in order: lanes of one
 // digit find each other by ballots, and the wave's own counter of the digit
 // gives the place of the first of them.
+template <int ITEMS>
 __global__ __launch_bounds__(kThreads) void radix_place_kernel(RadixArgs a) {
-  constexpr int kWaves = kThreads / kWave;
+  if (other_work(a.list)) return;
   // Lanes of a wave read what others of it wrote: volatile keeps every access.
   __shared__ volatile uint32_t count[kWaves][kDigits];
   __shared__ uint32_t base[kDigits];
   __shared__ uint32_t lds[kWaves];
   const int digits = 1 << a.bits;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) count[i / kDigits][i % kDigits] = 0;
-  {  // where each digit's entries begin
-    constexpr int kPer = kDigits / kThreads;
-    uint32_t v[kPer], sum = 0, all;
+  const int64_t first = (int64_t)blockIdx.x * kTile<ITEMS> + wave * (ITEMS * kWave);
+  int2 e[ITEMS];
+  int digit[ITEMS];
+  uint32_t place[ITEMS];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = threadIdx.x * kPer + k;
-      v[k] = i < digits ? a.totals[i] : 0;
-      sum += v[k];
-    }
-    uint32_t at = scan_threads(sum, lds, &all);
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int i = threadIdx.x * kPer + k;
-      base[i] = at + (i < digits ? a.counts[(int64_t)i * a.tiles + blockIdx.x] : 0);
-      at += v[k];
-    }
-  }
-  __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * kTile + wave * (kTileItems * kWave);
-  int2 e[kTileItems];
-  int digit[kTileItems];
-  uint32_t place[kTileItems];
-#pragma unroll
-  for (int k = 0; k < kTileItems; ++k) {
+  for (int k = 0; k < ITEMS; ++k) {
     const int64_t i = first + k * kWave + lane;
     digit[k] = -1;
     if (i < a.list.tokens) {
@@ -433,8 +454,28 @@ __global__ __launch_bounds__(kThreads) void radix_place_kernel(RadixArgs a) {
       digit[k] = (e[k].x >> a.shift) & (digits - 1);
     }
   }
+  for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) count[i / kDigits][i % kDigits] = 0;
+  {  // where each digit's entries begin
+    constexpr int kPer = kDigits / kThreads;
+    uint32_t v[kPer], before[kPer], sum = 0, all;
 #pragma unroll
-  for (int k = 0; k < kTileItems; ++k) {
+    for (int k = 0; k < kPer; ++k) {
+      const int i = threadIdx.x * kPer + k;
+      v[k] = i < digits ? a.totals[i] : 0;
+      before[k] = i < digits ? a.counts[(int64_t)i * a.tiles + blockIdx.x] : 0;
+      sum += v[k];
+    }
+    uint32_t at = scan_threads(sum, lds, &all);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int i = threadIdx.x * kPer + k;
+      base[i] = at + before[k];
+      at += v[k];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
     const bool valid = digit[k] >= 0;
     unsigned long long same = __ballot(valid);
     for (int bit = 0; bit < a.bits; ++bit) {
@@ -451,7 +492,7 @@ __global__ __launch_bounds__(kThreads) void radix_place_kernel(RadixArgs a) {
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kTileItems; ++k)
+  for (int k = 0; k < ITEMS; ++k)
     if (digit[k] >= 0) {
       uint32_t at = base[digit[k]] + place[k];
       for (int w = 0; w < wave; ++w) at += count[w][digit[k]];
@@ -473,9 +514,14 @@ struct SumArgs {
   double scale;
   void *out;
   int64_t out_rows;
-  double *slots;  // [chunk][2][dim]: the sum of the chunk's first row, if it began before
-                  // the chunk, and of its last one, if that goes on behind it
+  void *slots;  // Slot<type> [chunk][2][dim]: the sum of the chunk's first row, if it began
+                // before the chunk, and of its last one, if that goes on behind it
 };
+// Partial sums of a row: double, and float where the row is rounded to 16 bits in the
+// end, 2^-24 of them against its 2^-9 or 2^-12 (half the bytes, a tenth of all that
+// the sum over 262144 tokens of 512 float16 values moves).
+template <class T>
+using Slot = std::conditional_t<sizeof(T) == 2, float, double>;
 
 constexpr int kSumRows = 8;  // of a lane group in flight
 
@@ -506,22 +552,27 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
   auto slot = [&](int which) {
-    double *s = a.slots + (q * 2 + which) * a.dim + c;
+    Slot<T> *s = static_cast<Slot<T> *>(a.slots) + (q * 2 + which) * a.dim + c;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) s[i] = acc[i];
+    for (int i = 0; i < VEC; ++i) s[i] = (Slot<T>)acc[i];
   };
+  int2 next[kSumRows];  // the entries of the next rows are read while these arrive
+#pragma unroll
+  for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p0 + k, p1 - 1)];
   for (int64_t p = p0; p < p1; p += kSumRows) {
     int2 e[kSumRows];
     T v[kSumRows][VEC];
     double w[kSumRows];
 #pragma unroll
-    for (int k = 0; k < kSumRows; ++k) e[k] = a.entries[min(p + k, p1 - 1)];
+    for (int k = 0; k < kSumRows; ++k) e[k] = next[k];
 #pragma unroll
     for (int k = 0; k < kSumRows; ++k) {
       const int r = max(e[k].y, 0);
       load_vals<T, VEC>(src + (int64_t)r * a.src_stride + c, v[k]);
       w[k] = a.src_weights ? a.src_weights[r] : 1.0;
     }
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p + kSumRows + k, p1 - 1)];
 #pragma unroll
     for (int k = 0; k < kSumRows; ++k) {
       if (p + k >= p1) break;
@@ -549,45 +600,90 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
     slot(0);
 }
 
-// Rows that cross chunks: the workgroup of the chunk where the row began adds its
-// partial sums, the chunks' in order over the lane groups, the groups' in order.
-constexpr int kJoinCols = 64;  // columns of a workgroup
+// Rows that cross chunks: the wave of the chunk where the row began adds its partial
+// sums in the chunks' order, VEC columns a lane; those of a row of more than
+// kJoinAlone chunks are shared by the workgroup's waves, every kWaves-th each, and
+// the waves' sums are added in order.
+constexpr int kJoinAlone = 24;
+constexpr int kJoinDepth = 8;  // partial sums in flight
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a) {
-  constexpr int GPB = kThreads / kJoinCols;
-  __shared__ double part[GPB][kJoinCols];
-  const int64_t q = blockIdx.x, p0 = q * a.chunk, p1 = p0 + a.chunk;
-  if (p1 >= a.n) return;
-  const int key = a.entries[p1].x;
-  if (a.entries[p1 - 1].x != key || key >= a.out_rows || key < 0) return;
-  if (p0 > 0 && a.entries[p0 - 1].x == key) return;  // it began before
-  // Chunks q + 1 .. last begin in the row.
-  const int lane = threadIdx.x % kWave;
-  int64_t last = q;
-  for (;;) {
+// The sum of chunks k0, k0 + step, .. last of the row that began in chunk q.
+template <class S, int VEC>
+__device__ __forceinline__ void add_slots(const SumArgs &a, int c, int64_t q, int64_t k0,
+                                          int64_t last, int step, double (&acc)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+  for (int64_t k = k0; k <= last; k += step * kJoinDepth) {
+    S v[kJoinDepth][VEC];
+#pragma unroll
+    for (int u = 0; u < kJoinDepth; ++u) {
+      const int64_t m = min(k + u * step, last);
+      load_vals<S, VEC>(static_cast<const S *>(a.slots) + (m * 2 + (m == q ? 1 : 0)) * a.dim + c, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kJoinDepth; ++u)
+      if (k + u * step <= last) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += (double)v[u][i];
+      }
+  }
+}
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a, int64_t chunks) {
+  __shared__ double part[kWaves][kWave * VEC];
+  __shared__ int64_t first[kWaves], end[kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int c0 = blockIdx.y * (kWave * VEC) + lane * VEC;
+  const bool active = c0 < a.dim;
+  const int c = active ? min(c0, a.dim - VEC) : 0;
+  const int64_t q = (int64_t)blockIdx.x * kWaves + wave;
+  const int64_t p0 = q * a.chunk, p1 = p0 + a.chunk;
+  bool mine = q < chunks && p1 < a.n;  // uniform in the wave, as all that follows from it
+  int key = 0;
+  if (mine) {
+    key = a.entries[p1].x;
+    const int before = p0 > 0 ? a.entries[p0 - 1].x : -1;
+    mine = a.entries[p1 - 1].x == key && key < a.out_rows && before != key;
+  }
+  int64_t last = q;  // chunks q + 1 .. last begin in the row
+  while (mine) {
     const int64_t at = (last + 1 + lane) * a.chunk;
     const unsigned long long in = __ballot(at < a.n && a.entries[min(at, a.n - 1)].x == key);
-    if (in == ~0ull) {
-      last += kWave;
-    } else {
+    if (in != ~0ull) {
       last += __builtin_ctzll(~in);
       break;
     }
+    last += kWave;
   }
-  const int grp = threadIdx.x / kJoinCols, col = threadIdx.x % kJoinCols;
-  const int c = blockIdx.y * kJoinCols + col;
-  const bool active = c < a.dim;
-  double acc = 0.0;
-  if (active)
-    for (int64_t k = q + grp; k <= last; k += GPB)
-      acc += a.slots[(k * 2 + (k == q ? 1 : 0)) * a.dim + c];
-  part[grp][col] = acc;
+  double acc[VEC];
+  const bool alone = mine && last - q < kJoinAlone;
+  if (alone && active) {
+    add_slots<Slot<T>, VEC>(a, c, q, q, last, 1, acc);
+    write_row<T, VEC>(a, key, c, acc);
+  }
+  if (lane == 0) {
+    first[wave] = mine && !alone ? q : -1;
+    end[wave] = last;
+  }
   __syncthreads();
-  if (grp != 0 || !active) return;
-  for (int k = 1; k < GPB; ++k) acc += part[k][col];
-  const double sum[1] = {acc};
-  write_row<T, 1>(a, key, c, sum);
+  for (int w = 0; w < kWaves; ++w) {
+    const int64_t q0 = first[w];  // the same for the whole workgroup
+    if (q0 < 0) continue;
+    add_slots<Slot<T>, VEC>(a, c, q0, q0 + wave, end[w], kWaves, acc);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) part[wave][lane * VEC + i] = acc[i];
+    __syncthreads();
+    if (wave == w && active) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        acc[i] = part[0][lane * VEC + i];
+        for (int k = 1; k < kWaves; ++k) acc[i] += part[k][lane * VEC + i];
+      }
+      write_row<T, VEC>(a, key, c, acc);
+    }
+    __syncthreads();
+  }
 }
 
 // -- how a call is launched ----------------------------------------------------------------
@@ -602,7 +698,7 @@ int lanes_for(int32_t dim, int vec) {
 // f(T{}, vec, lanes) for the type and width of a call's rows, as constants.
 template <class T, class F>
 void with_lanes(int32_t dim, F f) {
-  constexpr int V = Row<T>::kVec;
+  constexpr int V = kVec<T>;
   const bool wide = dim >= V;
   const int lpg = lanes_for(dim, wide ? V : 1);
   auto go = [&](auto lanes) {
@@ -631,7 +727,9 @@ void with_rows(kbc_type type, int32_t dim, F f) {
 }
 
 // Entries of a chunk: about 4096 waves' worth of lane groups over the list, at
-// least kSumRows entries each.
+// least kSumRows entries each (262144 tokens of 512 float16 values: gradient 154 us;
+// with 2048 waves 183, with 8192 164, which leave too little in flight or too many
+// partial sums).
 int32_t chunk_for(int64_t tokens, int lpg) {
   int32_t chunk = kSumRows;
   while (chunk < 128 && tokens * lpg > (int64_t)chunk * 4096 * kWave) chunk *= 2;
@@ -654,12 +752,12 @@ Scratch scratch_for(int64_t tokens, int64_t bags, int32_t dim, bool sorted, bool
   s.entries = take(tokens * 8);
   if (sorted && tokens > kRankTokens) {
     s.sorted = take(tokens * 8);
-    s.counts = take((int64_t)kDigits * ceil_div(tokens, kTile) * 4);
+    s.counts = take(kDigits * tiles_of(tokens) * 4);
     s.totals = take(kDigits * 4);
   }
   if (mean) s.weights = take(bags * 8);
   const int64_t chunks = ceil_div(tokens, chunk_for(tokens, lpg));
-  if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);
+  if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);  // (half of it with 16-bit types)
   s.bytes = at;
   return s;
 }
@@ -683,19 +781,31 @@ void launch_sum(kbc_type type, const SumArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((sum_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
   });
   if (chunks <= 1) return;
-  const dim3 grid((unsigned)chunks, (unsigned)ceil_div(a.dim, kJoinCols));
+  auto join = [&](auto t) {
+    using T = decltype(t);
+    const unsigned wgs = (unsigned)ceil_div(chunks, kWaves);
+    if (a.dim >= 2)
+      hipLaunchKernelGGL((join_kernel<T, 2>), dim3(wgs, (unsigned)ceil_div(a.dim, kWave * 2)),
+                         dim3(kThreads), 0, s, a, chunks);
+    else
+      hipLaunchKernelGGL((join_kernel<T, 1>), dim3(wgs), dim3(kThreads), 0, s, a, chunks);
+  };
   switch (type) {
-    case KBC_F32: hipLaunchKernelGGL(join_kernel<float>, grid, dim3(kThreads), 0, s, a); break;
-    case KBC_BF16: hipLaunchKernelGGL(join_kernel<__bf16>, grid, dim3(kThreads), 0, s, a); break;
-    case KBC_F16: hipLaunchKernelGGL(join_kernel<_Float16>, grid, dim3(kThreads), 0, s, a); break;
+    case KBC_F32: join(float{}); break;
+    case KBC_BF16: join(__bf16{}); break;
+    case KBC_F16: join(_Float16{}); break;
   }
 }
 
-// The grid of a list's first launch, and which of its workgroups do what.
-dim3 list_grid(ListArgs *a, int64_t list_wgs) {
+// The grid of launch k of `launches` that make a list: the first also weighs the
+// bags, and each clears a share of the output.
+dim3 list_grid(ListArgs *a, int64_t list_wgs, int k, int launches) {
+  const int64_t pieces = ceil_div(a->fill_bytes, kFillBytes);
+  const int64_t from = pieces * k / launches, to = pieces * (k + 1) / launches;
   a->list_wgs = (uint32_t)list_wgs;
-  a->weight_wgs = a->mean ? (uint32_t)ceil_div(a->bags.n, kThreads / kWave) : 0;
-  return dim3((unsigned)(list_wgs + a->weight_wgs + ceil_div(a->fill_bytes, kFillBytes)));
+  a->weight_wgs = k == 0 && a->mean ? (uint32_t)ceil_div(a->bags.n, kWaves) : 0;
+  a->first_fill = (uint32_t)from;
+  return dim3((unsigned)(list_wgs + a->weight_wgs + to - from));
 }
 
 bool bad_sizes(int64_t tokens, int64_t bags, int64_t rows, int32_t dim, int32_t id_bytes) {
@@ -764,12 +874,12 @@ kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int
   if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
   char *w = static_cast<char *>(scratch);
   ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, reinterpret_cast<double *>(w + at.weights),
-             out, bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0};
-  const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads));
+             out, bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
+  const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads), 0, 1);
   hipLaunchKernelGGL(pool_list_kernel, grid, dim3(kThreads), 0, s, l);
   const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), table, stride, dim, nullptr,
                   mean ? l.weights : nullptr, scale, out, bags,
-                  reinterpret_cast<double *>(w + at.slots)};
+                  w + at.slots};
   launch_sum(type, a, s);
   return launched();
 }
@@ -796,28 +906,31 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
   char *w = static_cast<char *>(scratch);
   ListArgs l{{ids, id_bytes}, bags_of(bags, offsets, id_bytes, tokens), tokens, rows, mean,
              reinterpret_cast<double *>(w + at.weights), dtable, rows * dim * size_of(type),
-             reinterpret_cast<int2 *>(w + at.entries), 0, 0};
+             reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
   if (tokens <= kRankTokens) {
-    const dim3 grid = list_grid(&l, ceil_div(tokens, kRankPer));
+    const dim3 grid = list_grid(&l, ceil_div(tokens, kRankPer), 0, 1);
     hipLaunchKernelGGL(rank_kernel, grid, dim3(kThreads), (size_t)ceil_div(tokens, 4) * 16, s, l);
   } else {
     int bits = 1;
     while ((rows >> bits) != 0) ++bits;  // keys are 0 .. rows
     const int passes = (int)ceil_div(bits, kDigitBits);
-    RadixArgs r{l, nullptr, nullptr, 0, 0, (uint32_t)ceil_div(tokens, kTile),
+    RadixArgs r{l, nullptr, nullptr, 0, 0, (uint32_t)tiles_of(tokens),
                 reinterpret_cast<uint32_t *>(w + at.counts),
                 reinterpret_cast<uint32_t *>(w + at.totals)};
     int2 *to[2] = {l.entries, reinterpret_cast<int2 *>(w + at.sorted)};
     for (int p = 0; p < passes; ++p) {
       r.bits = (bits - r.shift + (passes - p) - 1) / (passes - p);
       r.out = to[(passes - 1 - p) % 2];  // the last pass writes the entries
-      dim3 grid(r.tiles);
-      r.list.list_wgs = r.tiles;
-      if (p == 0) grid = list_grid(&r.list, r.tiles);
-      hipLaunchKernelGGL(radix_count_kernel, grid, dim3(kThreads), 0, s, r);
-      hipLaunchKernelGGL(radix_scan_kernel, dim3(1u << r.bits), dim3(kThreads), 0, s, r.tiles,
-                         r.counts, r.totals);
-      hipLaunchKernelGGL(radix_place_kernel, dim3(r.tiles), dim3(kThreads), 0, s, r);
+      auto grid = [&](int64_t wgs, int k) { return list_grid(&r.list, wgs, p * 3 + k, passes * 3); };
+      const dim3 count = grid(r.tiles, 0);
+      const bool long_list = tokens >= kLongList;
+      hipLaunchKernelGGL(long_list ? radix_count_kernel<8> : radix_count_kernel<2>, count,
+                         dim3(kThreads), 0, s, r);
+      const dim3 scan = grid(int64_t(1) << r.bits, 1);
+      hipLaunchKernelGGL(radix_scan_kernel, scan, dim3(kThreads), 0, s, r);
+      const dim3 place = grid(r.tiles, 2);
+      hipLaunchKernelGGL(long_list ? radix_place_kernel<8> : radix_place_kernel<2>, place,
+                         dim3(kThreads), 0, s, r);
       r.in = r.out;
       r.shift += r.bits;
     }
@@ -825,7 +938,7 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
   if (tokens > 0) {
     const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), dout, dim, dim,
                     mean ? l.weights : nullptr, nullptr, scale, dtable, rows,
-                    reinterpret_cast<double *>(w + at.slots)};
+                    w + at.slots};
     launch_sum(type, a, s);
   }
   return launched();

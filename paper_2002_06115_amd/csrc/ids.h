@@ -49,6 +49,24 @@ __device__ __forceinline__ int64_t bag_of(const Bags &b, int64_t t) {
   return lo >= 1 && lo <= b.n ? lo - 1 : -1;
 }
 
+// The same by L neighbouring lanes for a token of theirs, L + 1 parts a step.
+template <int L>
+__device__ __forceinline__ int64_t bag_of_lanes(const Bags &b, int64_t t, int lane) {
+  if (!b.offsets.p) return t / b.each;
+  int64_t lo = 0, hi = b.n + 1;
+  while (lo < hi) {
+    const int64_t step = (hi - lo + L) / (L + 1);
+    const int64_t at = lo + step * (lane + 1) - 1;  // the last of the lane's part
+    const bool below = at < hi && bag_begin(b, at) <= t;
+    const unsigned long long mask = __ballot(below) >> (threadIdx.x % kWave / L * L) & ((1ull << L) - 1);
+    const int parts = __popcll(mask);  // that end at or before t
+    const int64_t from = lo + parts * step;
+    if (parts < L && hi > from + step - 1) hi = from + step - 1;
+    lo = from;
+  }
+  return lo >= 1 && lo <= b.n ? lo - 1 : -1;
+}
+
 // -- host side ----------------------------------------------------------------------
 
 inline Bags bags_of(int64_t bags, const void *offsets, int32_t id_bytes, int64_t tokens) {

@@ -5,7 +5,9 @@ Tolerances.  A sum of n terms in double is off by at most n 2^-53 times the sum 
 its terms' sizes, below 1e-10 of it here, and the output is rounded to float (2^-24
 of the value) and, in a 16-bit type, once more (2^-9 bfloat16 at its spacing of 2^-8,
 2^-12 float16 at 2^-11, counted as half a step: 2^-8 and 2^-11 relative at most;
-below its smallest normal number, half of float16's step 2^-24).
+below its smallest normal number, half of float16's step 2^-24).  In a 16-bit type the
+partial sums of a row that crosses chunks are rounded to float on the way: 2^-24 of
+each, together at most 2^-24 of the sum of the terms' sizes.
 """
 import ctypes
 
@@ -65,7 +67,8 @@ def close(got, want, sums, dtype, what):
     got = got.double().cpu().numpy()
     assert got.shape == want.shape, what
     least = 2.0 ** -25 if dtype == "float16" else 0.0
-    bound = (ROUND[dtype] + 2.0 ** -23) * np.abs(want) + 1e-10 * sums + least
+    rest = 1e-10 if dtype == "float32" else 1e-10 + 2.0 ** -24
+    bound = (ROUND[dtype] + 2.0 ** -23) * np.abs(want) + rest * sums + least
     bad = ~(np.abs(got - want) <= bound)
     assert not bad.any(), f"{what}: {int(bad.sum())} values off, first at {np.argwhere(bad)[0]}"
 
