@@ -267,40 +267,36 @@ kb_status kb_follow_accumulate(const kb_t *kb, int32_t b, const float *X, const 
  *
  * kb_pack keeps row j of X [rows][b] as 8-bit floats (e4m3: 4 exponent and 3 mantissa
  * bits, no infinities) of X[j] / 2^e, rounded to nearest even, with an exponent of
- * its own: the smallest e >= -127 with |x| <= 448 * 2^e for every finite x of the row.
+ * its own: the smallest e >= -126 with |x| <= 448 * 2^e for every finite x of the row.
  * kb_unpack gives the values kept, code * 2^e, exactly: off by at most 2^-4 of the
  * value, or 2^-10 * 2^e where that is more (2^e is at most 1 / 224 of the row's
- * largest size, unless e is -127); sizes over 248 * 2^120, which would round past the
+ * largest size, unless e is -126); sizes over 248 * 2^120, which would round past the
  * largest float, are kept as 240 * 2^120.  Infinities and NaN are kept as NaN and set
  * no exponent.
  *
- *   rows      : 0 .. 2^30.
- *   X         : DEVICE float [rows][b], aligned as for kb_follow.
- *   codes     : DEVICE bytes [rows][kb_packed_pitch(b)], 4-byte aligned from b = 4 on.
- *   exponents : DEVICE bytes [rows], e + 127.
- *   A row's codes are in an order of the library's own (at widths that are not a
- *   multiple of 4 some twice).  The three arrays must not overlap.
+ *   rows   : 0 .. 2^30.
+ *   X      : DEVICE float [rows][b], aligned as for kb_follow.
+ *   packed : DEVICE [rows][kb_packed_pitch(b)] bytes, 4-byte aligned, codes and exponents
+ *            in an order of the library's own (36 bytes a row at b = 32, 16 at b = 10).
+ *   X and packed must not overlap.
  * Work is enqueued on `stream` of the current device.  KB_EINVAL as for kb_follow.
  */
 size_t kb_packed_pitch(int32_t b);
-kb_status kb_pack(int64_t rows, int32_t b, const float *X, uint8_t *codes, uint8_t *exponents,
-                  void *stream);
-kb_status kb_unpack(int64_t rows, int32_t b, const uint8_t *codes, const uint8_t *exponents,
-                    float *X, void *stream);
+kb_status kb_pack(int64_t rows, int32_t b, const float *X, void *packed, void *stream);
+kb_status kb_unpack(int64_t rows, int32_t b, const void *packed, float *X, void *stream);
 
 /*
  * kb_follow_backward and kb_follow_backward_residual for X [N_E][b] as kb_pack kept
- * it (codes and exponents, never NULL): the dR pass reads the kept values, dX needs
- * none.  Other arguments, rules, workspace and errors as there.
+ * it (never NULL): the dR pass reads the kept values, dX needs none.  Other arguments,
+ * rules, workspace and errors as there.
  */
-kb_status kb_follow_backward_packed(const kb_t *kb, int32_t b, const uint8_t *codes,
-                                    const uint8_t *exponents, const float *R, const float *dY,
-                                    float *dX, float *dR, void *workspace, size_t ws_bytes,
-                                    void *stream);
-kb_status kb_follow_backward_residual_packed(const kb_t *kb, int32_t b, const uint8_t *codes,
-                                             const uint8_t *exponents, const float *R,
-                                             const float *dY, float gamma, float *dX, float *dR,
-                                             void *workspace, size_t ws_bytes, void *stream);
+kb_status kb_follow_backward_packed(const kb_t *kb, int32_t b, const void *packed, const float *R,
+                                    const float *dY, float *dX, float *dR, void *workspace,
+                                    size_t ws_bytes, void *stream);
+kb_status kb_follow_backward_residual_packed(const kb_t *kb, int32_t b, const void *packed,
+                                             const float *R, const float *dY, float gamma,
+                                             float *dX, float *dR, void *workspace,
+                                             size_t ws_bytes, void *stream);
 
 /* Static description of a status code. */
 const char *kb_status_str(kb_status s);

@@ -81,13 +81,13 @@ def _load_library():
     lib.kb_follow_backward_residual.restype = ctypes.c_int
     lib.kb_packed_pitch.argtypes = [i32]
     lib.kb_packed_pitch.restype = sz
-    lib.kb_pack.argtypes = [i64, i32, p, p, p, p]
+    lib.kb_pack.argtypes = [i64, i32, p, p, p]
     lib.kb_pack.restype = ctypes.c_int
-    lib.kb_unpack.argtypes = [i64, i32, p, p, p, p]
+    lib.kb_unpack.argtypes = [i64, i32, p, p, p]
     lib.kb_unpack.restype = ctypes.c_int
-    lib.kb_follow_backward_packed.argtypes = [p, i32, p, p, p, p, p, p, p, sz, p]
+    lib.kb_follow_backward_packed.argtypes = [p, i32, p, p, p, p, p, p, sz, p]
     lib.kb_follow_backward_packed.restype = ctypes.c_int
-    lib.kb_follow_backward_residual_packed.argtypes = [p, i32, p, p, p, p, f32, p, p, p, sz, p]
+    lib.kb_follow_backward_residual_packed.argtypes = [p, i32, p, p, p, f32, p, p, p, sz, p]
     lib.kb_follow_backward_residual_packed.restype = ctypes.c_int
     lib.kb_status_str.argtypes = [ctypes.c_int]
     lib.kb_status_str.restype = ctypes.c_char_p
@@ -176,53 +176,50 @@ def _on_device(fn, what, device, *args):
 
 
 class Packed:
-    """Entity sets [rows][b] kept in 8 bits (pack): e4m3 codes and an exponent a row."""
+    """Entity sets [rows][b] kept in 8 bits (pack): data [rows][pitch] uint8, the
+    library's own layout of e4m3 codes and an exponent a row."""
 
-    def __init__(self, codes, exponents, b):
+    def __init__(self, data, b):
         import torch
-        for t, name, dims in ((codes, "codes", 2), (exponents, "exponents", 1)):
-            if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_cuda:
-                raise TypeError(f"{name} must be a uint8 CUDA tensor")
-            if t.dim() != dims or not t.is_contiguous() or t.device != codes.device or \
-                    t.shape[0] != codes.shape[0]:
-                raise ValueError("codes and exponents must be contiguous, a row and a byte a set")
-        if b < 1 or codes.shape[1] != _lib.kb_packed_pitch(int(b)):
-            raise ValueError(f"codes are not those of rows of {b} values")
-        self.codes, self.exponents, self.b = codes, exponents, int(b)
+        if not isinstance(data, torch.Tensor) or data.dtype != torch.uint8 or not data.is_cuda:
+            raise TypeError("data must be a uint8 CUDA tensor")
+        if b < 1 or data.dim() != 2 or data.shape[1] != _lib.kb_packed_pitch(int(b)) or \
+                not data.is_contiguous():
+            raise ValueError(f"data must be contiguous packed rows of {b} values")
+        self.data, self.b = data, int(b)
 
     @property
     def shape(self):
-        return self.codes.shape[0], self.b
+        return self.data.shape[0], self.b
 
     @property
     def device(self):
-        return self.codes.device
+        return self.data.device
 
     def unpack(self):
         """The values kept, float32 [rows][b]."""
         import torch
         X = torch.empty(self.shape, dtype=torch.float32, device=self.device)
-        _on_device(_lib.kb_unpack, "kb_unpack", self.device, self.codes.shape[0], self.b,
-                   self.codes.data_ptr(), self.exponents.data_ptr(), X.data_ptr())
+        _on_device(_lib.kb_unpack, "kb_unpack", self.device, self.data.shape[0], self.b,
+                   self.data.data_ptr(), X.data_ptr())
         return X
 
 
 def pack(X):
-    """X [rows][b] kept in 8 bits, a quarter of the memory: row j as 8-bit floats (e4m3,
-    rounded to nearest even) of X[j] / 2^e, e the smallest exponent from -127 on with
-    |x| <= 448 * 2^e for every finite x of the row.  A kept value is off by at most
-    2^-4 of itself, or 2^-10 * 2^e; infinities are kept as NaN."""
+    """X [rows][b] kept in 8 bits: row j as 8-bit floats (e4m3, rounded to nearest even)
+    of X[j] / 2^e, e the smallest exponent from -126 on with |x| <= 448 * 2^e for every
+    finite x of the row.  A kept value is off by at most 2^-4 of itself, or 2^-10 * 2^e;
+    infinities are kept as NaN.  0.28 of the memory where b is a multiple of 32 (0.4
+    at b = 10)."""
     import torch
     if not isinstance(X, torch.Tensor) or X.dtype != torch.float32 or not X.is_cuda:
         raise TypeError("X must be a float32 CUDA tensor")
     if X.dim() != 2 or X.shape[1] < 1 or not X.is_contiguous():
         raise ValueError("X must be a contiguous [rows][b] tensor")
     rows, b = X.shape
-    codes = torch.empty((rows, _lib.kb_packed_pitch(b)), dtype=torch.uint8, device=X.device)
-    exponents = torch.empty(rows, dtype=torch.uint8, device=X.device)
-    _on_device(_lib.kb_pack, "kb_pack", X.device, rows, b, X.data_ptr(), codes.data_ptr(),
-               exponents.data_ptr())
-    return Packed(codes, exponents, b)
+    data = torch.empty((rows, _lib.kb_packed_pitch(b)), dtype=torch.uint8, device=X.device)
+    _on_device(_lib.kb_pack, "kb_pack", X.device, rows, b, X.data_ptr(), data.data_ptr())
+    return Packed(data, b)
 
 
 class KB:
@@ -396,16 +393,15 @@ class KB:
         dX = self._act(dX, self.n_entities, "dX") if want_dx else None
         dR = self._act(dR, self.n_relations, "dR") if want_dr else None
         if packed is not None:
-            kept = packed.codes.data_ptr(), packed.exponents.data_ptr()
             if residual is None:
                 self._enqueue(_lib.kb_follow_backward_packed, "kb_follow_backward_packed", stream,
-                              b, *kept, self._ptr(R), self._ptr(dY), self._ptr(dX),
-                              self._ptr(dR))
+                              b, self._ptr(packed.data), self._ptr(R), self._ptr(dY),
+                              self._ptr(dX), self._ptr(dR))
             else:
                 self._enqueue(_lib.kb_follow_backward_residual_packed,
-                              "kb_follow_backward_residual_packed", stream, b, *kept,
-                              self._ptr(R), self._ptr(dY), float(residual), self._ptr(dX),
-                              self._ptr(dR))
+                              "kb_follow_backward_residual_packed", stream, b,
+                              self._ptr(packed.data), self._ptr(R), self._ptr(dY),
+                              float(residual), self._ptr(dX), self._ptr(dR))
         elif residual is None:
             self._enqueue(_lib.kb_follow_backward, "kb_follow_backward", stream, b, self._ptr(X),
                           self._ptr(R), self._ptr(dY), self._ptr(dX), self._ptr(dR))
@@ -474,19 +470,16 @@ def _make_functions():
             ctx.kb = kb
             ctx.residual = residual
             ctx.b = X.shape[-1]
-            kept = (None, None)
-            if ctx.needs_input_grad[1]:
-                P = pack(X)
-                kept = P.codes, P.exponents
-            ctx.save_for_backward(*kept, R if ctx.needs_input_grad[0] else None)
+            ctx.save_for_backward(pack(X).data if ctx.needs_input_grad[1] else None,
+                                  R if ctx.needs_input_grad[0] else None)
             return kb.follow(X, R, residual=residual)
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dY):
-            codes, exponents, R = ctx.saved_tensors
+            data, R = ctx.saved_tensors
             need_x, need_r = ctx.needs_input_grad[0], ctx.needs_input_grad[1]
-            X = Packed(codes, exponents, ctx.b) if need_r else None
+            X = Packed(data, ctx.b) if need_r else None
             dX, dR = ctx.kb.follow_backward(X, R, dY.contiguous(), want_dx=need_x,
                                             want_dr=need_r, residual=ctx.residual)
             return dX, dR, None, None
@@ -507,8 +500,8 @@ def _follow_fn(pack):
 def follow(kb: KB, X, R, pack: bool = False):
     """Differentiable follow(X, R) (Eq. 4) on entity-major tensors X [N_E][b], R [N_R][b].
 
-    With ``pack`` the backward pass keeps X in 8 bits (a quarter of the memory):
-    R's gradient is that of the values kept (see pack()), X's is the same."""
+    With ``pack`` X is kept in 8 bits for the backward pass (see pack()):
+    R's gradient is that of the values kept, X's is the same."""
     return _follow_fn(pack).apply(X, R, kb, None)
 
 

@@ -294,12 +294,12 @@ kb_status run_sweep(const kb_t *kb, const DevLayout &D, int ph_base, int32_t b, 
 // Runs one pass after its sweep: the stream kernel, the first combine level
 // together with the empty rows (unless swept), the further combine levels.
 // With Z non-null (one row per output row; A itself for the residual hop, out
-// itself to add in place) every output row j also gets gamma * Z[j].  With codes
-// non-null B is packed (launch_packed), and Z is null.
+// itself to add in place) every output row j also gets gamma * Z[j].  With packed
+// non-null B is that (launch_packed), and Z is null.
 kb_status run_pass(const kb_t *kb, const DevLayout &D, int ph_base, const float *A,
                    int64_t A_rows, const float *B, int64_t B_rows, int32_t b, float *out,
                    void *ws, const float *Z, float gamma, bool swept, hipStream_t s,
-                   const uint8_t *codes = nullptr, const uint8_t *exponents = nullptr) {
+                   const uint8_t *packed = nullptr) {
   double *slots = static_cast<double *>(ws);
   const float *res = Z;
   if (D.n > 0) {
@@ -316,8 +316,9 @@ kb_status run_pass(const kb_t *kb, const DevLayout &D, int ph_base, const float 
     o.n_cu = kb->n_cu;
     o.max_lpt = lane_cap(kb, ph_base, b);
     hipError_t e =
-        codes ? launch_packed({a, codes, exponents}, o, s, scope.launch_start(), scope.launch_stop())
-              : launch_stream(a, o, s, scope.launch_start(), scope.launch_stop());
+        packed ? launch_packed({a, packed, (uint32_t)packed_pitch(b)}, o, s, scope.launch_start(),
+                               scope.launch_stop())
+               : launch_stream(a, o, s, scope.launch_start(), scope.launch_stop());
     if (e != hipSuccess) return hip_fail(e, "stream kernel launch");
   }
   {
@@ -657,11 +658,11 @@ kb_status follow_impl(const kb_t *kb, int32_t b, const float *X, const float *R,
   }
 }
 
-// X as floats, or with codes non-null packed.
+// X as floats, or with packed non-null as that.
 kb_status backward_impl(const kb_t *kb, int32_t b, const float *X, const float *R,
                         const float *dY, bool residual, float gamma, float *dX, float *dR,
                         void *workspace, size_t ws_bytes, void *stream,
-                        const uint8_t *codes = nullptr, const uint8_t *exponents = nullptr) {
+                        const uint8_t *packed = nullptr) {
   try {
     if (!kb) return fail(KB_EINVAL, "kb must be non-NULL");
     if (b < 1) return fail(KB_EINVAL, "b must be >= 1");
@@ -671,12 +672,10 @@ kb_status backward_impl(const kb_t *kb, int32_t b, const float *X, const float *
     const bool want_dr = dR != nullptr && rel_bytes > 0;
     if ((want_dx || want_dr) && ent_bytes && !dY) return fail(KB_EINVAL, "dY must be non-NULL");
     if (want_dx && rel_bytes && !R) return fail(KB_EINVAL, "R must be non-NULL to compute dX");
-    const size_t code_bytes = codes ? (size_t)kb->n_entities * (size_t)packed_pitch(b) : 0;
-    const size_t exp_bytes = codes ? (size_t)kb->n_entities : 0;
-    if (want_dr && ent_bytes && !X && !codes)
+    const size_t packed_bytes = packed ? (size_t)kb->n_entities * (size_t)packed_pitch(b) : 0;
+    if (want_dr && ent_bytes && !X && !packed)
       return fail(KB_EINVAL, "X must be non-NULL to compute dR");
-    if (codes && b >= 4 && !aligned(codes, 4))
-      return fail(KB_EINVAL, "codes must be 4-byte aligned");
+    if (packed && !aligned(packed, 4)) return fail(KB_EINVAL, "the packed X must be 4-byte aligned");
     const size_t al = (b % 4 == 0) ? 16 : 4;
     for (const void *p : {(const void *)X, (const void *)R, (const void *)dY, (const void *)dX,
                           (const void *)dR})
@@ -688,16 +687,13 @@ kb_status backward_impl(const kb_t *kb, int32_t b, const float *X, const float *
     if (want_dr && (overlaps(dR, rel_bytes, X, ent_bytes) || overlaps(dR, rel_bytes, R, rel_bytes) ||
                     overlaps(dR, rel_bytes, dY, ent_bytes)))
       return fail(KB_EINVAL, "dR overlaps another array");
-    if (want_dx && (overlaps(dX, ent_bytes, codes, code_bytes) ||
-                    overlaps(dX, ent_bytes, exponents, exp_bytes)))
-      return fail(KB_EINVAL, "dX overlaps the packed X");
-    if (want_dr && (overlaps(dR, rel_bytes, codes, code_bytes) ||
-                    overlaps(dR, rel_bytes, exponents, exp_bytes)))
-      return fail(KB_EINVAL, "dR overlaps the packed X");
+    if ((want_dx && overlaps(dX, ent_bytes, packed, packed_bytes)) ||
+        (want_dr && overlaps(dR, rel_bytes, packed, packed_bytes)))
+      return fail(KB_EINVAL, "dX or dR overlaps the packed X");
     kb_status st = check_ws(workspace_bytes(kb, b), workspace, ws_bytes,
                             {{X, ent_bytes}, {R, rel_bytes}, {dY, ent_bytes},
                              {want_dx ? dX : nullptr, ent_bytes}, {want_dr ? dR : nullptr, rel_bytes},
-                             {codes, code_bytes}, {exponents, exp_bytes}});
+                             {packed, packed_bytes}});
     if (st != KB_OK) return st;
     if ((st = check_device(kb)) != KB_OK) return st;
     g_last_error.clear();
@@ -744,7 +740,7 @@ kb_status backward_impl(const kb_t *kb, int32_t b, const float *X, const float *
     if (st == KB_OK && want_dr) {
       // By relation, runs of equal subject: dR[k] = sum over runs of X[s] (.) sum of dY[o].
       st = run_pass(kb, kb->L[BY_REL], KB_PH_DR_STREAM, dY, kb->n_entities, X, kb->n_entities,
-                    b, dR, dr_ws, nullptr, 0.0f, dr_swept, dr_s, codes, exponents);
+                    b, dR, dr_ws, nullptr, 0.0f, dr_swept, dr_s, packed);
     }
     if (overlap) {
       // Joined whatever happened above, so the caller's stream never runs
@@ -827,21 +823,19 @@ size_t kb_packed_pitch(int32_t b) { return b < 1 ? 0 : (size_t)packed_pitch(b); 
 namespace {
 
 // The checks that kb_pack and kb_unpack share; *nothing says that there is no row.
-kb_status check_packing(int64_t rows, int32_t b, const void *X, const void *codes,
-                        const void *exponents, bool *nothing) {
+kb_status check_packing(int64_t rows, int32_t b, const void *X, const void *packed,
+                        bool *nothing) {
   *nothing = rows == 0;
   if (rows < 0 || rows > (int64_t(1) << 30)) return fail(KB_EINVAL, "rows must be 0 .. 2^30");
   if (b < 1) return fail(KB_EINVAL, "b must be >= 1");
   if (rows == 0) return KB_OK;
-  if (!X || !codes || !exponents) return fail(KB_EINVAL, "X, codes and exponents must be non-NULL");
+  if (!X || !packed) return fail(KB_EINVAL, "X and packed must be non-NULL");
   if (!aligned(X, b % 4 == 0 ? 16 : 4))
     return fail(KB_EINVAL, "X must be " + std::to_string(b % 4 == 0 ? 16 : 4) + "-byte aligned");
-  if (b >= 4 && !aligned(codes, 4)) return fail(KB_EINVAL, "codes must be 4-byte aligned");
-  const size_t x_bytes = (size_t)rows * (size_t)b * sizeof(float);
-  const size_t code_bytes = (size_t)rows * (size_t)packed_pitch(b);
-  if (overlaps(X, x_bytes, codes, code_bytes) || overlaps(X, x_bytes, exponents, (size_t)rows) ||
-      overlaps(codes, code_bytes, exponents, (size_t)rows))
-    return fail(KB_EINVAL, "X, codes and exponents overlap");
+  if (!aligned(packed, 4)) return fail(KB_EINVAL, "packed must be 4-byte aligned");
+  if (overlaps(X, (size_t)rows * (size_t)b * sizeof(float), packed,
+               (size_t)rows * (size_t)packed_pitch(b)))
+    return fail(KB_EINVAL, "X and packed overlap");
   return KB_OK;
 }
 
@@ -849,56 +843,51 @@ kb_status check_packing(int64_t rows, int32_t b, const void *X, const void *code
 
 extern "C" {
 
-kb_status kb_pack(int64_t rows, int32_t b, const float *X, uint8_t *codes, uint8_t *exponents,
-                  void *stream) {
+kb_status kb_pack(int64_t rows, int32_t b, const float *X, void *packed, void *stream) {
   try {
     bool nothing = false;
-    const kb_status st = check_packing(rows, b, X, codes, exponents, &nothing);
+    const kb_status st = check_packing(rows, b, X, packed, &nothing);
     if (st != KB_OK) return st;
     g_last_error.clear();
     if (nothing) return KB_OK;
-    const hipError_t e =
-        launch_pack(X, rows, b, codes, exponents, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_pack(X, rows, b, static_cast<uint8_t *>(packed),
+                                     static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KB_OK : hip_fail(e, "pack kernel launch");
   } catch (...) {
     return fail(KB_EINVAL, "unexpected host error");
   }
 }
 
-kb_status kb_unpack(int64_t rows, int32_t b, const uint8_t *codes, const uint8_t *exponents,
-                    float *X, void *stream) {
+kb_status kb_unpack(int64_t rows, int32_t b, const void *packed, float *X, void *stream) {
   try {
     bool nothing = false;
-    const kb_status st = check_packing(rows, b, X, codes, exponents, &nothing);
+    const kb_status st = check_packing(rows, b, X, packed, &nothing);
     if (st != KB_OK) return st;
     g_last_error.clear();
     if (nothing) return KB_OK;
-    const hipError_t e =
-        launch_unpack(codes, exponents, rows, b, X, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_unpack(static_cast<const uint8_t *>(packed), rows, b, X,
+                                       static_cast<hipStream_t>(stream));
     return e == hipSuccess ? KB_OK : hip_fail(e, "unpack kernel launch");
   } catch (...) {
     return fail(KB_EINVAL, "unexpected host error");
   }
 }
 
-kb_status kb_follow_backward_packed(const kb_t *kb, int32_t b, const uint8_t *codes,
-                                    const uint8_t *exponents, const float *R, const float *dY,
-                                    float *dX, float *dR, void *workspace, size_t ws_bytes,
-                                    void *stream) {
-  if (kb && kb->n_entities > 0 && (!codes || !exponents))
-    return fail(KB_EINVAL, "codes and exponents must be non-NULL");
+kb_status kb_follow_backward_packed(const kb_t *kb, int32_t b, const void *packed, const float *R,
+                                    const float *dY, float *dX, float *dR, void *workspace,
+                                    size_t ws_bytes, void *stream) {
+  if (kb && kb->n_entities > 0 && !packed) return fail(KB_EINVAL, "packed must be non-NULL");
   return backward_impl(kb, b, nullptr, R, dY, false, 0.0f, dX, dR, workspace, ws_bytes, stream,
-                       codes, exponents);
+                       static_cast<const uint8_t *>(packed));
 }
 
-kb_status kb_follow_backward_residual_packed(const kb_t *kb, int32_t b, const uint8_t *codes,
-                                             const uint8_t *exponents, const float *R,
-                                             const float *dY, float gamma, float *dX, float *dR,
-                                             void *workspace, size_t ws_bytes, void *stream) {
-  if (kb && kb->n_entities > 0 && (!codes || !exponents))
-    return fail(KB_EINVAL, "codes and exponents must be non-NULL");
+kb_status kb_follow_backward_residual_packed(const kb_t *kb, int32_t b, const void *packed,
+                                             const float *R, const float *dY, float gamma,
+                                             float *dX, float *dR, void *workspace,
+                                             size_t ws_bytes, void *stream) {
+  if (kb && kb->n_entities > 0 && !packed) return fail(KB_EINVAL, "packed must be non-NULL");
   return backward_impl(kb, b, nullptr, R, dY, true, gamma, dX, dR, workspace, ws_bytes, stream,
-                       codes, exponents);
+                       static_cast<const uint8_t *>(packed));
 }
 
 kb_status kb_checked_violations(uint64_t *count, int32_t reset) {

@@ -100,21 +100,25 @@ hipError_t launch_stream(const StreamArgs &a, const StreamOptions &o, hipStream_
 std::string describe_stream(const StreamArgs &a, const StreamOptions &o);
 
 // Entity sets kept in 8 bits (packed): row j of X [rows][b] as e4m3 codes of
-// X[j] / 2^e, with e = exponents[j] - 127 the smallest exponent for which no code
-// overflows (|x| <= 448 * 2^e), but at least -127.  A row's codes are whole dwords from
-// 4 columns on, dword k those of columns min(4 k, b - 4) on: what lane k of a lane
-// group works on (LaneCols), so a ragged row's last dword repeats some.
-inline int64_t packed_pitch(int32_t b) { return b < 4 ? b : ((int64_t)b + 3) / 4 * 4; }
-hipError_t launch_pack(const float *X, int64_t rows, int32_t b, uint8_t *codes,
-                       uint8_t *exponents, hipStream_t s);
-hipError_t launch_unpack(const uint8_t *codes, const uint8_t *exponents, int64_t rows, int32_t b,
-                         float *X, hipStream_t s);
+// X[j] / 2^e, with e the smallest exponent for which no code overflows (|x| <= 448 *
+// 2^e), but at least -126.  From 4 columns on a row is dwords: 2^e as a float before
+// every kPackedLanes dwords of four codes, dword k of those being columns min(4 k, b - 4)
+// on, what lane k of a lane group works on (LaneCols; so a ragged row's last dword
+// repeats some).  Narrower rows are b codes and the byte e + 127, in 2 or 4 bytes.
+constexpr int kPackedLanes = 8;
+inline int64_t packed_pitch(int32_t b) {
+  if (b < 4) return b == 1 ? 2 : 4;
+  const int64_t lanes = ((int64_t)b + 3) / 4;
+  return 4 * (lanes + (lanes + kPackedLanes - 1) / kPackedLanes);
+}
+hipError_t launch_pack(const float *X, int64_t rows, int32_t b, uint8_t *packed, hipStream_t s);
+hipError_t launch_unpack(const uint8_t *packed, int64_t rows, int32_t b, float *X, hipStream_t s);
 // launch_stream with B packed (the dR pass with X kept in 8 bits): s.B is not
 // read, and s.residual is 0.
 struct PackedArgs {
   StreamArgs s;
-  const uint8_t *codes;
-  const uint8_t *exponents;
+  const uint8_t *rows;  // of pitch bytes, packed_pitch(b)
+  uint32_t pitch;
 };
 hipError_t launch_packed(const PackedArgs &a, const StreamOptions &o, hipStream_t s,
                          hipEvent_t start = nullptr, hipEvent_t stop = nullptr);

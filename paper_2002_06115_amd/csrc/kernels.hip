@@ -55,6 +55,10 @@ typedef float kbf_float4 __attribute__((ext_vector_type(4)));
 __device__ kbf_float4 struct_buffer_load_f32x4(__amdgpu_buffer_rsrc_t rsrc, int idx, int off,
                                                int soff, int aux)
     __asm("llvm.amdgcn.struct.ptr.buffer.load.v4f32");
+typedef int kbf_int2 __attribute__((ext_vector_type(2)));
+__device__ kbf_int2 struct_buffer_load_i32x2(__amdgpu_buffer_rsrc_t rsrc, int idx, int off,
+                                             int soff, int aux)
+    __asm("llvm.amdgcn.struct.ptr.buffer.load.v2i32");
 
 namespace kbf {
 
@@ -808,35 +812,41 @@ __global__ __launch_bounds__(kBlock) void narrow_kernel(StreamArgs a) {
 
 // -- entity sets in 8 bits ------------------------------------------------------
 //
-// The dR pass with X as launch_pack left it: the stream kernel without its
-// residual and LDS forms, a run's B row decoded when it starts,
-//     held = decode(codes[b_id]) * 2^(exponents[b_id] - 127),
-// which is exact (4 significant bits, within a float's range), so dR is the sum over
-// the kept values with one rounding, as from a float X.  The exponents of a step's
-// run starts are read by the lanes that fetched the entries, one load for all, and
-// shared like the entries.
+// The dR pass with X as launch_pack left it (kernels.h): the stream kernel without
+// its residual and LDS forms.  A run's B row comes with its scale in one 8-byte load
+// a lane: the dword before the lane's codes, which is the scale for the first lane of
+// eight and is handed to the others by a swizzle, as the entries are.  What is held is
+// the dword of codes and the scale, decoded for every entry by the two instructions
+// that apply a scale while they convert, so an entry costs the lanes no more than
+// from floats.  Decoding is exact (4 significant bits, within a float's range): dR is
+// the sum over the kept values with one rounding, as from a float X.
 //
-// LANE: 4 floats per lane, kRaggedLane likewise, or 1 (rows of less than 4 floats).
+// A scale in an array of its own would be one more line per run start (10 M entities,
+// b = 32, dR 969 us; float X 757).
+//
+// LANE: 4 floats per lane, or kRaggedLane likewise.
 
-// The four values of a dword of codes, times 2^e.
-__device__ __forceinline__ void decode4(uint32_t codes, int e, float (&v)[4]) {
-  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false);
-  const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
-  v[0] = __builtin_ldexpf(lo[0], e);
-  v[1] = __builtin_ldexpf(lo[1], e);
-  v[2] = __builtin_ldexpf(hi[0], e);
-  v[3] = __builtin_ldexpf(hi[1], e);
+typedef kbf_int2 int2_any __attribute__((aligned(4)));
+
+// The four values of a dword of codes, times the scale.
+__device__ __forceinline__ void decode4(uint32_t codes, float scale, float (&v)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false);
+  const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+  v[0] = lo[0];
+  v[1] = lo[1];
+  v[2] = hi[0];
+  v[3] = hi[1];
 }
-__device__ __forceinline__ float decode1(uint32_t code, int e) {
-  return __builtin_ldexpf(__builtin_amdgcn_cvt_f32_fp8((int)code, 0), e);
+// Where lane k of a row's lanes finds (the dword before, its codes).
+__device__ __forceinline__ uint32_t packed_offset(uint32_t k) {
+  return 4 * (k + k / kPackedLanes);
 }
-constexpr int kPackBias = 127;
 
 template <int LANE, int LPT, bool BUF, bool WEIGHTED>
 __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
   constexpr bool RAGGED = LANE == kRaggedLane;
-  constexpr int VEC = RAGGED ? 4 : LANE;
-  static_assert(VEC == 4 || !BUF, "narrow rows take plain loads");
+  constexpr int VEC = 4;
+  constexpr int SHARE = LPT < kPackedLanes ? LPT : kPackedLanes;  // lanes of one scale
   const StreamArgs &a = pa.s;
   constexpr int GPB = kBlock / LPT;
   const int lane = threadIdx.x % LPT;
@@ -846,9 +856,7 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
   const int c = lane_cols<RAGGED>(c0, a.b).c;
   const size_t bb = (size_t)a.b;
   const int cl = active ? c : 0;
-  // Where the lane's codes are in a row of them: its dword, or its byte.
-  const int kl = active ? c0 : 0;
-  const size_t pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
+  const uint32_t code_bytes = active ? packed_offset((uint32_t)c0 / VEC) : 0;
   const uint32_t row_bytes = (uint32_t)a.b * (uint32_t)sizeof(float);
   const uint32_t col_bytes = (uint32_t)cl * (uint32_t)sizeof(float);
   auto rsrc = [](const void *p, uint64_t bytes, int stride) {
@@ -856,7 +864,7 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
                                              (int)(uint32_t)bytes, kRawBufferWord3);
   };
   const __amdgpu_buffer_rsrc_t arsrc = rsrc(a.A, (uint64_t)a.A_rows, (int)row_bytes);
-  const __amdgpu_buffer_rsrc_t brsrc = rsrc(pa.codes, (uint64_t)a.B_rows * pitch, 0);
+  const __amdgpu_buffer_rsrc_t brsrc = rsrc(pa.rows, (uint64_t)a.B_rows, (int)pa.pitch);
   const __amdgpu_buffer_rsrc_t orsrc = rsrc(a.out, (uint64_t)a.out_rows * row_bytes, 0);
   const __amdgpu_buffer_rsrc_t srsrc =
       rsrc(a.slots, (uint64_t)a.n_slots * a.b * sizeof(double), 0);
@@ -873,7 +881,9 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
   const int64_t wgs_in_list = ((int64_t)gridDim.x - xl + nl - 1) / nl;
   const int64_t stride = wgs_in_list * GPB;
 
+  // Entries as in the stream kernel, two steps' with one load where it takes them so.
   constexpr int K = (kUnroll + LPT - 1) / LPT;
+  constexpr bool kPairFetch = !WEIGHTED && LPT == kUnroll;
   auto fetch = [&](int64_t p, int2 (&mine)[K], float (&wmine)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -882,37 +892,44 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
       if constexpr (WEIGHTED) wmine[k] = a.weights[q];
     }
   };
+  auto fetch2 = [&](int64_t p, int4 &mine) {
+    const int64_t q = min(p + 2 * min(lane, kUnroll - 1), a.n - 2);
+    mine = reinterpret_cast<const int4 *>(a.entries)[q / 2];
+  };
 
   for (int64_t g = c_begin + (blockIdx.x / nl) * GPB + grp; g < c_end; g += stride) {
     const int64_t p0 = KBF_CHECKED(g, a.n / a.chunk) * a.chunk;
     const int64_t p1 = p0 + a.chunk;
     double acc[VEC];
-    float held_b[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      acc[v] = 0.0;
-      held_b[v] = 0.0f;
-    }
-    int2 mine[K];
-    float wmine[K];
-    fetch(p0, mine, wmine);
-    for (int64_t p = p0; p < p1; p += kUnroll) {
+    for (int v = 0; v < VEC; ++v) acc[v] = 0.0;
+    int held = 0, held_scale = 0;  // the current run's codes and scale
+    int2 mine_next[K];
+    float wmine_next[K];
+    int4 mine2 = make_int4(0, 0, 0, 0);
+    if constexpr (kPairFetch)
+      fetch2(p0, mine2);
+    else
+      fetch(p0, mine_next, wmine_next);
+    auto step = [&](const int64_t p, auto hc) {
+      constexpr int H = decltype(hc)::value;
       int2 e[kUnroll];
       float w[kUnroll];
       float xa[kUnroll][VEC];
-      uint32_t xb[kUnroll];
-      int exps[K];
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const bool start = mine[k].x >= 0 && (mine[k].x & kRunStart);
-        exps[k] = pa.exponents[start ? KBF_CHECKED(mine[k].y & kIdMask, a.B_rows) : 0];
-      }
+      kbf_int2 xb[kUnroll];  // (the dword before, codes)
       static_for<kUnroll>([&](auto uc) {
         constexpr int u = decltype(uc)::value;
-        const int2 m = mine[u / LPT];
-        e[u] = make_int2(group_bcast<LPT, u % LPT>(m.x), group_bcast<LPT, u % LPT>(m.y));
-        if constexpr (WEIGHTED)
-          w[u] = __int_as_float(group_bcast<LPT, u % LPT>(__float_as_int(wmine[u / LPT])));
+        if constexpr (H >= 0) {
+          constexpr int src = (kUnroll / 2) * H + u / 2;
+          const int ex = (u % 2) ? mine2.z : mine2.x;
+          const int ey = (u % 2) ? mine2.w : mine2.y;
+          e[u] = make_int2(group_bcast<LPT, src>(ex), group_bcast<LPT, src>(ey));
+        } else {
+          const int2 m = mine_next[u / LPT];
+          e[u] = make_int2(group_bcast<LPT, u % LPT>(m.x), group_bcast<LPT, u % LPT>(m.y));
+          if constexpr (WEIGHTED)
+            w[u] = __int_as_float(group_bcast<LPT, u % LPT>(__float_as_int(wmine_next[u / LPT])));
+        }
       });
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
@@ -921,51 +938,47 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
         const bool same_a = u > 0 && triple && (e[u].y & kSameA);
         const int32_t ia = e[u].x & kIdMask, ib = e[u].y & kIdMask;
         if constexpr (BUF) {
-          gather_row(arsrc, triple && !same_a ? (uint32_t)KBF_CHECKED(ia, a.A_rows) : kNoRecord,
-                     col_bytes, xa[u]);
-          xb[u] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(
-              brsrc,
-              (int)(run_start ? (uint32_t)KBF_CHECKED(ib, a.B_rows) * (uint32_t)pitch + (uint32_t)kl
-                              : kOutOfRange),
+#if defined(KBFOLLOW_CHECKED)
+          const uint32_t ra = (triple && !same_a) ? (uint32_t)KBF_CHECKED(ia, a.A_rows) : kNoRecord;
+#else
+          const uint32_t ra = same_a ? kNoRecord : ((uint32_t)e[u].x & ~(uint32_t)kRunStart);
+#endif
+          gather_row(arsrc, ra, col_bytes, xa[u]);
+          xb[u] = struct_buffer_load_i32x2(
+              brsrc, run_start ? (int)KBF_CHECKED(ib, a.B_rows) : (int)kNoRecord, (int)code_bytes,
               0, 0);
         } else {
           load_row<VEC>(a.A + (size_t)(triple ? KBF_CHECKED(ia, a.A_rows) : 0) * bb + cl, xa[u]);
-          const uint8_t *row =
-              pa.codes + (size_t)(run_start ? KBF_CHECKED(ib, a.B_rows) : 0) * pitch + kl;
-          if constexpr (VEC == 4)
-            xb[u] = *reinterpret_cast<const uint32_t *>(row);
-          else
-            xb[u] = *row;
+          xb[u] = *reinterpret_cast<const int2_any *>(
+              pa.rows + (size_t)(run_start ? KBF_CHECKED(ib, a.B_rows) : 0) * pa.pitch + code_bytes);
         }
       }
-      int e_mine[K];
-#pragma unroll
-      for (int k = 0; k < K; ++k) e_mine[k] = exps[k] - kPackBias;
-      fetch(p + kUnroll, mine, wmine);
+      if constexpr (H < 0)
+        fetch(p + kUnroll, mine_next, wmine_next);
+      else if constexpr (H == 1)
+        fetch2(p + kUnroll, mine2);
       static_for<kUnroll>([&](auto uc) {
         constexpr int u = decltype(uc)::value;
         const bool triple = e[u].x >= 0;
         const bool run_start = triple && (e[u].x & kRunStart);
-        if constexpr (BUF) {
-          if constexpr (u > 0) {
-            const bool same_a = triple && (e[u].y & kSameA);
+        if constexpr (BUF && u > 0) {
+          const bool same_a = triple && (e[u].y & kSameA);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) xa[u][v] = same_a ? xa[u - 1][v] : xa[u][v];
-          }
+          for (int v = 0; v < VEC; ++v) xa[u][v] = same_a ? xa[u - 1][v] : xa[u][v];
         }
-        const int eb = group_bcast<LPT, u % LPT>(e_mine[u / LPT]);
-        float nb[VEC];
-        if constexpr (VEC == 4)
-          decode4(xb[u], eb, nb);
-        else
-          nb[0] = decode1(xb[u], eb);
+        // Run starts take the new row, markers zeros (their loads' with BUF).
+        const int scale = group_bcast<SHARE, 0>(xb[u][0]);
+        const bool take = run_start || !triple;
+        held = take ? ((BUF || triple) ? xb[u][1] : 0) : held;
+        held_scale = take ? scale : held_scale;
+        float b4[VEC];
+        decode4((uint32_t)held, __int_as_float(held_scale), b4);
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          held_b[v] = run_start ? nb[v] : triple ? held_b[v] : 0.0f;
           double t = (double)xa[u][v];
           if constexpr (WEIGHTED) t *= (double)w[u];
           if constexpr (!BUF) t = triple ? t : 0.0;
-          acc[v] = __builtin_fma(t, (double)held_b[v], acc[v]);
+          acc[v] = __builtin_fma(t, (double)b4[v], acc[v]);
         }
         const int f = e[u].y;
         if (!triple) {
@@ -991,131 +1004,286 @@ __global__ __launch_bounds__(kBlock) void packed_kernel(PackedArgs pa) {
           for (int v = 0; v < VEC; ++v) acc[v] = 0.0;
         }
       });
+    };
+    if constexpr (kPairFetch) {
+      for (int64_t p = p0; p < p1; p += 2 * kUnroll) {
+        step(p, std::integral_constant<int, 0>{});
+        if (p + kUnroll >= p1) break;
+        step(p + kUnroll, std::integral_constant<int, 1>{});
+      }
+    } else {
+      for (int64_t p = p0; p < p1; p += kUnroll) step(p, std::integral_constant<int, -1>{});
     }
   }
 }
 
-// The exponent byte of a row whose largest finite size has the bits `top`:
-// 448 = 1.75 * 2^8, so from the exponent 8 less, 7 where the mantissa passes 1.75.
+// Rows of at most kMaxNarrow floats, as in narrow_kernel: a lane per entry, its
+// packed row and the scale in one load.
+template <int N>
+__device__ __forceinline__ void load_packed(const uint8_t *row, float (&v)[N]) {
+  if constexpr (N == 1) {
+    const uint32_t x = *reinterpret_cast<const uint16_t *>(row);
+    v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, __int_as_float((int)(x >> 8 << 23)), false)[0];
+  } else if constexpr (N < 4) {
+    const uint32_t x = *reinterpret_cast<const uint32_t *>(row);
+    const float scale = __int_as_float((int)((x >> 8 * N & 0xFF) << 23));
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, scale, false);
+    v[0] = lo[0];
+    v[1] = lo[1];
+    if constexpr (N == 3) v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, scale, true)[0];
+  } else {
+    const kbf_int2 x = *reinterpret_cast<const int2_any *>(row);
+    decode4((uint32_t)x[1], __int_as_float(x[0]), v);
+  }
+}
+
+template <int N, bool WEIGHTED>
+__global__ __launch_bounds__(kBlock) void narrow_packed_kernel(PackedArgs pa) {
+  const StreamArgs &a = pa.s;
+  constexpr int U = N <= 2 ? 2 * kNarrowSteps : kNarrowSteps;
+  const int l = threadIdx.x % kNarrowLanes;
+  constexpr int GPB = kBlock / kNarrowLanes;
+
+  const int nl = a.n_lists;
+  const int xl = (int)(blockIdx.x % (unsigned)nl);
+  int64_t c_begin = 0, c_end = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxChunkLists; ++i)
+    if (i == xl) {
+      c_begin = a.list_chunk[i];
+      c_end = a.list_chunk[i + 1];
+    }
+  const int64_t wgs_in_list = ((int64_t)gridDim.x - xl + nl - 1) / nl;
+  const int64_t stride = wgs_in_list * GPB;
+
+  const int steps = a.chunk / kNarrowLanes;
+  for (int64_t g = c_begin + (blockIdx.x / nl) * GPB + threadIdx.x / kNarrowLanes; g < c_end;
+       g += stride) {
+    const int64_t p0 = KBF_CHECKED(g, a.n / a.chunk) * a.chunk + l;
+    auto entry = [&](int s, int2 &e, float &w) {
+      if (s < steps) {
+        e = a.entries[p0 + s * kNarrowLanes];
+        if constexpr (WEIGHTED) w = a.weights[p0 + s * kNarrowLanes];
+      } else {  // past the chunk: markers of no target
+        e = make_int2(-1, INT_MIN);
+        w = 0.0f;
+      }
+    };
+    int2 next[U];
+    float wnext[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) entry(u, next[u], wnext[u]);
+    double prev[N];       // the previous step's scan
+    bool carry = false;   // its last lane's row goes on
+#pragma unroll
+    for (int v = 0; v < N; ++v) prev[v] = 0.0;
+
+    for (int s0 = 0; s0 < steps; s0 += U) {
+      int2 e[U];
+      float w[U];
+      float xa[U][N], xb[U][N];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        e[u] = next[u];
+        w[u] = wnext[u];
+        const bool triple = e[u].x >= 0;
+        const int32_t ia = triple ? (e[u].x & kIdMask) : 0;
+        const int32_t ib = triple ? (e[u].y & kIdMask) : 0;
+        load_floats<N>(a.A + (size_t)KBF_CHECKED(ia, a.A_rows) * N, xa[u]);
+        load_packed<N>(pa.rows + (size_t)KBF_CHECKED(ib, a.B_rows) * pa.pitch, xb[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) entry(s0 + U + u, next[u], wnext[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool triple = e[u].x >= 0;
+        const unsigned marks =
+            (unsigned)(__ballot(!triple) >> (threadIdx.x % 64 / kNarrowLanes * kNarrowLanes)) &
+            ((1u << kNarrowLanes) - 1);
+        const unsigned below = marks & ((1u << l) - 1);
+        const int start = below ? 32 - __builtin_clz(below) : 0;
+        double sum[N];
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+          double t = (double)xa[u][v];
+          if constexpr (WEIGHTED) t *= (double)w[u];
+          sum[v] = triple ? t * (double)xb[u][v] : 0.0;
+          const double c = dpp_double<kDppHalfMirror>(prev[v]);
+          sum[v] += (l == 0 && carry) ? c : 0.0;
+        }
+        const bool in1 = l - 1 >= start, in2 = l - 2 >= start, in4 = l - 4 >= start;
+#pragma unroll
+        for (int v = 0; v < N; ++v) {
+          const double t1 = dpp_double<kDppRowShr + 1>(sum[v]);
+          sum[v] += in1 ? t1 : 0.0;
+          const double t2 = dpp_double<kDppRowShr + 2>(sum[v]);
+          sum[v] += in2 ? t2 : 0.0;
+          const double t4 = dpp_double<kDppRowShr + 4>(sum[v]);
+          sum[v] += in4 ? t4 : 0.0;
+          prev[v] = sum[v];
+        }
+        carry = !(marks >> (kNarrowLanes - 1) & 1);
+        const int f = e[u].y;
+        if (!triple && f != INT_MIN) {
+          if (f >= 0) {
+            float *out = a.out + (size_t)KBF_CHECKED(f, a.out_rows) * N;
+#pragma unroll
+            for (int v = 0; v < N; ++v) out[v] = (float)sum[v];
+          } else {
+            double *slot = a.slots + (size_t)KBF_CHECKED(-(f + 1), a.n_slots) * N;
+#pragma unroll
+            for (int v = 0; v < N; ++v) slot[v] = sum[v];
+          }
+        }
+      }
+    }
+  }
+}
+
+// The biased exponent of the scale of a row whose largest finite size has the bits
+// `top`: 448 = 1.75 * 2^8, so from the exponent 8 less, 7 where the mantissa passes
+// 1.75.  A scale is a normal float: its bits are its exponent's.
 __device__ __forceinline__ int pack_exponent(uint32_t top) {
-  return max(0, (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u));
+  return max(1, (int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u));
 }
 __device__ __forceinline__ uint32_t size_bits(float x) {
   const uint32_t u = __float_as_uint(x) & 0x7FFFFFFFu;
   return u < 0x7F800000u ? u : 0;  // infinities and NaN set no exponent
 }
 constexpr uint32_t kPackNaN = 0x7F;
-// The code of x / 2^e (e4m3 has no infinities: they are kept as NaN, as NaN is).
-// Under the largest exponent, 120, the code of 240 is the last whose value is a
+constexpr int kTopExponent = 247;
+// The code of x / scale (e4m3 has no infinities: they are kept as NaN, as NaN is).
+// Under the largest scale, 2^120, the code of 240 is the last whose value is a
 // float: 256 * 2^120, to which the largest floats would round, is not.
-__device__ __forceinline__ uint32_t encode1(float x, int e) {
+__device__ __forceinline__ uint32_t encode1(float x, int exponent) {
   const bool finite = (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u;
-  const float most = e == 120 ? 240.0f : 448.0f;
-  const float y = fminf(fmaxf(__builtin_ldexpf(finite ? x : 0.0f, -e), -most), most);
+  const float most = exponent == kTopExponent ? 240.0f : 448.0f;
+  const float y = fminf(fmaxf(__builtin_ldexpf(finite ? x : 0.0f, 127 - exponent), -most), most);
   const uint32_t code = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y, y, 0, false) & 0xFFu;
   return finite ? code : kPackNaN;
 }
 
-// A lane group of LPT lanes per row, kPackRows rows of it in flight; rows of
-// more than LPT vectors take a second look at what they read.  Bound by the bytes
-// moved: a float read, a byte written (and the other way round).
+// A lane group of LPT lanes per row, kPackRows rows of it in flight, the rows of
+// neighbouring groups side by side; rows of more than LPT vectors take a second look
+// at what they read.  Bound by the bytes moved.
 constexpr int kPackRows = 4;
 
-template <int VEC, int LPT>
+template <int LPT>
 __global__ __launch_bounds__(kBlock) void pack_kernel(const float *__restrict__ X, int64_t rows,
-                                                      int32_t b, uint8_t *__restrict__ codes,
-                                                      uint8_t *__restrict__ exponents) {
+                                                      int32_t b, uint32_t pitch,
+                                                      uint8_t *__restrict__ packed) {
   constexpr int GPB = kBlock / LPT;
   const int lane = threadIdx.x % LPT;
-  const int64_t r0 = ((int64_t)blockIdx.x * GPB + threadIdx.x / LPT) * kPackRows;
-  const size_t bb = (size_t)b, pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
-  auto col = [&](int c0) { return VEC == 4 ? min(c0, b - 4) : c0; };
-  float x[kPackRows][VEC];
-  uint32_t top[kPackRows];
+  const int64_t r0 = (int64_t)blockIdx.x * (GPB * kPackRows) + threadIdx.x / LPT;
+  const size_t bb = (size_t)b;
+  auto at = [&](int k, int c0) {
+    return X + (size_t)min(r0 + k * GPB, rows - 1) * bb + min(c0, b - 4);
+  };
+  float x[kPackRows][4];
 #pragma unroll
   for (int k = 0; k < kPackRows; ++k) {
-    const int64_t r = min(r0 + k, rows - 1);
-    top[k] = 0;
-    if (lane * VEC < b) {
-      load_row<VEC>(X + (size_t)r * bb + col(lane * VEC), x[k]);
+    if (lane * 4 < b) {
+      load_row<4>(at(k, lane * 4), x[k]);
     } else {
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) x[k][v] = 0.0f;
+      for (int v = 0; v < 4; ++v) x[k][v] = 0.0f;
     }
+  }
+  int exponent[kPackRows];
+#pragma unroll
+  for (int k = 0; k < kPackRows; ++k) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) top = max(top, size_bits(x[k][v]));
+    for (int64_t c0 = (int64_t)(lane + LPT) * 4; c0 < b; c0 += LPT * 4) {
+      float y[4];
+      load_row<4>(at(k, (int)c0), y);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) top = max(top, size_bits(y[v]));
+    }
+#pragma unroll
+    for (int m = 1; m < LPT; m <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    exponent[k] = pack_exponent(top);
   }
 #pragma unroll
   for (int k = 0; k < kPackRows; ++k) {
-    const int64_t r = min(r0 + k, rows - 1);
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) top[k] = max(top[k], size_bits(x[k][v]));
-    for (int64_t c0 = (int64_t)(lane + LPT) * VEC; c0 < b; c0 += LPT * VEC) {
-      float y[VEC];
-      load_row<VEC>(X + (size_t)r * bb + col((int)c0), y);
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) top[k] = max(top[k], size_bits(y[v]));
-    }
-#pragma unroll
-    for (int m = 1; m < LPT; m <<= 1) top[k] = max(top[k], (uint32_t)__shfl_xor((int)top[k], m));
-  }
-#pragma unroll
-  for (int k = 0; k < kPackRows; ++k) {
-    const int64_t r = r0 + k;
+    const int64_t r = r0 + k * GPB;
     if (r >= rows) break;
-    const int byte = pack_exponent(top[k]), e = byte - kPackBias;
-    if (lane == 0) exponents[r] = (uint8_t)byte;
-    auto put = [&](int c0, const float (&y)[VEC]) {
-      uint8_t *at = codes + (size_t)r * pitch + c0;
-      if constexpr (VEC == 4)
-        *reinterpret_cast<uint32_t *>(at) = encode1(y[0], e) | encode1(y[1], e) << 8 |
-                                            encode1(y[2], e) << 16 | encode1(y[3], e) << 24;
-      else
-        *at = (uint8_t)encode1(y[0], e);
+    auto put = [&](int c0, const float (&y)[4]) {
+      const uint32_t n = (uint32_t)c0 / 4;
+      uint32_t *to = reinterpret_cast<uint32_t *>(packed + (size_t)r * pitch + packed_offset(n));
+      if (n % kPackedLanes == 0) to[0] = (uint32_t)exponent[k] << 23;
+      to[1] = encode1(y[0], exponent[k]) | encode1(y[1], exponent[k]) << 8 |
+              encode1(y[2], exponent[k]) << 16 | encode1(y[3], exponent[k]) << 24;
     };
-    if (lane * VEC < b) put(lane * VEC, x[k]);
-    for (int64_t c0 = (int64_t)(lane + LPT) * VEC; c0 < b; c0 += LPT * VEC) {
-      float y[VEC];
-      load_row<VEC>(X + (size_t)r * bb + col((int)c0), y);
+    if (lane * 4 < b) put(lane * 4, x[k]);
+    for (int64_t c0 = (int64_t)(lane + LPT) * 4; c0 < b; c0 += LPT * 4) {
+      float y[4];
+      load_row<4>(at(k, (int)c0), y);
       put((int)c0, y);
     }
   }
 }
 
-template <int VEC, int LPT>
-__global__ __launch_bounds__(kBlock) void unpack_kernel(const uint8_t *__restrict__ codes,
-                                                        const uint8_t *__restrict__ exponents,
-                                                        int64_t rows, int32_t b,
+template <int LPT>
+__global__ __launch_bounds__(kBlock) void unpack_kernel(const uint8_t *__restrict__ packed,
+                                                        int64_t rows, int32_t b, uint32_t pitch,
                                                         float *__restrict__ X) {
   constexpr int GPB = kBlock / LPT;
   const int lane = threadIdx.x % LPT;
-  const int64_t r0 = ((int64_t)blockIdx.x * GPB + threadIdx.x / LPT) * kPackRows;
-  const size_t bb = (size_t)b, pitch = VEC == 4 ? (bb + 3) / 4 * 4 : bb;
-  int e[kPackRows];
-#pragma unroll
-  for (int k = 0; k < kPackRows; ++k) e[k] = (int)exponents[min(r0 + k, rows - 1)] - kPackBias;
-  for (int64_t c0 = (int64_t)lane * VEC; c0 < b; c0 += LPT * VEC) {
-    uint32_t x[kPackRows];
+  const int64_t r0 = (int64_t)blockIdx.x * (GPB * kPackRows) + threadIdx.x / LPT;
+  for (int64_t c0 = (int64_t)lane * 4; c0 < b; c0 += LPT * 4) {
+    const uint32_t n = (uint32_t)c0 / 4, own = packed_offset(n) + 4;
+    const uint32_t first = packed_offset(n / kPackedLanes * kPackedLanes);  // its scale's place
+    uint32_t code[kPackRows], scale[kPackRows];
 #pragma unroll
     for (int k = 0; k < kPackRows; ++k) {
-      const uint8_t *at = codes + (size_t)min(r0 + k, rows - 1) * pitch + c0;
-      if constexpr (VEC == 4)
-        x[k] = *reinterpret_cast<const uint32_t *>(at);
-      else
-        x[k] = *at;
+      const uint8_t *row = packed + (size_t)min(r0 + k * GPB, rows - 1) * pitch;
+      code[k] = *reinterpret_cast<const uint32_t *>(row + own);
+      scale[k] = *reinterpret_cast<const uint32_t *>(row + first);
     }
 #pragma unroll
     for (int k = 0; k < kPackRows; ++k) {
-      if (r0 + k >= rows) break;
-      float *to = X + (size_t)(r0 + k) * bb + (VEC == 4 ? min((int)c0, b - 4) : (int)c0);
-      if constexpr (VEC == 4) {
-        float v[4];
-        decode4(x[k], e[k], v);
-        const double d[4] = {v[0], v[1], v[2], v[3]};
-        store_row<4>(to, d);
-      } else {
-        *to = decode1(x[k], e[k]);
-      }
+      const int64_t r = r0 + k * GPB;
+      if (r >= rows) break;
+      float v[4];
+      decode4(code[k], __uint_as_float(scale[k]), v);
+      const float4_any y = {v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<float4_any *>(X + (size_t)r * b + min((int)c0, b - 4)) = y;
     }
   }
+}
+
+// Rows of less than 4 floats: a thread a row.
+template <int N>
+__global__ __launch_bounds__(kBlock) void pack_narrow_kernel(const float *__restrict__ X,
+                                                             int64_t rows, uint32_t pitch,
+                                                             uint8_t *__restrict__ packed) {
+  const int64_t r = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (r >= rows) return;
+  float x[N];
+  load_floats<N>(X + (size_t)r * N, x);
+  uint32_t top = 0, out = 0;
+#pragma unroll
+  for (int v = 0; v < N; ++v) top = max(top, size_bits(x[v]));
+  const int exponent = pack_exponent(top);
+#pragma unroll
+  for (int v = 0; v < N; ++v) out |= encode1(x[v], exponent) << 8 * v;
+  out |= (uint32_t)exponent << 8 * N;
+  if constexpr (N == 1)
+    *reinterpret_cast<uint16_t *>(packed + (size_t)r * pitch) = (uint16_t)out;
+  else
+    *reinterpret_cast<uint32_t *>(packed + (size_t)r * pitch) = out;
+}
+template <int N>
+__global__ __launch_bounds__(kBlock) void unpack_narrow_kernel(const uint8_t *__restrict__ packed,
+                                                               int64_t rows, uint32_t pitch,
+                                                               float *__restrict__ X) {
+  const int64_t r = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (r >= rows) return;
+  float x[N];
+  load_packed<N>(packed + (size_t)r * pitch, x);
+  __builtin_memcpy(X + (size_t)r * N, x, N * sizeof(float));
 }
 
 // Adds slots [first, first + n) in increasing order; writes the float row or
@@ -1684,61 +1852,72 @@ namespace {
 
 template <int LANE, bool BUF, bool WT>
 const void *packed_fn(int lpt) {
-  switch (lpt) {
-    case 1:
-      if constexpr (LANE == kRaggedLane)
-        return nullptr;
-      else
-        return reinterpret_cast<const void *>(&packed_kernel<LANE, 1, BUF, WT>);
-    case 2:
-      return reinterpret_cast<const void *>(&packed_kernel<LANE, 2, BUF, WT>);
-    case 4:
-      return reinterpret_cast<const void *>(&packed_kernel<LANE, 4, BUF, WT>);
-  }
-  if constexpr (LANE != 1) {
-    switch (lpt) {
-      case 8: return reinterpret_cast<const void *>(&packed_kernel<LANE, 8, BUF, WT>);
-      case 16: return reinterpret_cast<const void *>(&packed_kernel<LANE, 16, BUF, WT>);
-      case 32: return reinterpret_cast<const void *>(&packed_kernel<LANE, 32, BUF, WT>);
-    }
+  switch (lpt) {  // (rows of 5 floats or more: two lanes at least)
+    case 2: return reinterpret_cast<const void *>(&packed_kernel<LANE, 2, BUF, WT>);
+    case 4: return reinterpret_cast<const void *>(&packed_kernel<LANE, 4, BUF, WT>);
+    case 8: return reinterpret_cast<const void *>(&packed_kernel<LANE, 8, BUF, WT>);
+    case 16: return reinterpret_cast<const void *>(&packed_kernel<LANE, 16, BUF, WT>);
+    case 32: return reinterpret_cast<const void *>(&packed_kernel<LANE, 32, BUF, WT>);
   }
   return nullptr;
 }
 
-const void *packed_fn_for(const ColumnTiling &t, bool buf, bool wt) {
-  if (t.vec == 1) return wt ? packed_fn<1, false, true>(t.lpt) : packed_fn<1, false, false>(t.lpt);
-  if (t.ragged) {
+const void *packed_fn_for(bool ragged, int lpt, bool buf, bool wt) {
+  if (ragged) {
     if (buf)
-      return wt ? packed_fn<kRaggedLane, true, true>(t.lpt)
-                : packed_fn<kRaggedLane, true, false>(t.lpt);
-    return wt ? packed_fn<kRaggedLane, false, true>(t.lpt)
-              : packed_fn<kRaggedLane, false, false>(t.lpt);
+      return wt ? packed_fn<kRaggedLane, true, true>(lpt) : packed_fn<kRaggedLane, true, false>(lpt);
+    return wt ? packed_fn<kRaggedLane, false, true>(lpt) : packed_fn<kRaggedLane, false, false>(lpt);
   }
-  if (buf) return wt ? packed_fn<4, true, true>(t.lpt) : packed_fn<4, true, false>(t.lpt);
-  return wt ? packed_fn<4, false, true>(t.lpt) : packed_fn<4, false, false>(t.lpt);
+  if (buf) return wt ? packed_fn<4, true, true>(lpt) : packed_fn<4, true, false>(lpt);
+  return wt ? packed_fn<4, false, true>(lpt) : packed_fn<4, false, false>(lpt);
 }
 
-// f(vec, lanes) for rows of b floats, as constants.
+const void *narrow_packed_fn(int32_t b, bool wt) {
+  switch (b) {
+    case 1:
+      return wt ? reinterpret_cast<const void *>(&narrow_packed_kernel<1, true>)
+                : reinterpret_cast<const void *>(&narrow_packed_kernel<1, false>);
+    case 2:
+      return wt ? reinterpret_cast<const void *>(&narrow_packed_kernel<2, true>)
+                : reinterpret_cast<const void *>(&narrow_packed_kernel<2, false>);
+    case 3:
+      return wt ? reinterpret_cast<const void *>(&narrow_packed_kernel<3, true>)
+                : reinterpret_cast<const void *>(&narrow_packed_kernel<3, false>);
+    case 4:
+      return wt ? reinterpret_cast<const void *>(&narrow_packed_kernel<4, true>)
+                : reinterpret_cast<const void *>(&narrow_packed_kernel<4, false>);
+  }
+  return nullptr;
+}
+
+// f(lanes of a row, blocks) for rows of b >= 4 floats.
 template <class F>
-hipError_t with_pack_lanes(int32_t b, F f) {
-  const int lanes = b < 4 ? b : (b + 3) / 4;
+hipError_t with_pack_lanes(int64_t rows, int32_t b, F f) {
   int lpt = 1;
-  while (lpt < lanes && lpt < 64) lpt <<= 1;
-  if (b < 4) {
-    if (lpt == 1) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
-    if (lpt == 2) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 2>{});
-    return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-  }
-  constexpr std::integral_constant<int, 4> four{};
+  while (lpt * 4 < b && lpt < 64) lpt <<= 1;
+  const int64_t per = (int64_t)kBlock / lpt * kPackRows, blocks = (rows + per - 1) / per;
+  if (blocks * kBlock > (int64_t)UINT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
   switch (lpt) {
-    case 1: return f(four, std::integral_constant<int, 1>{});
-    case 2: return f(four, std::integral_constant<int, 2>{});
-    case 4: return f(four, std::integral_constant<int, 4>{});
-    case 8: return f(four, std::integral_constant<int, 8>{});
-    case 16: return f(four, std::integral_constant<int, 16>{});
-    case 32: return f(four, std::integral_constant<int, 32>{});
-    default: return f(four, std::integral_constant<int, 64>{});
+    case 1: f(std::integral_constant<int, 1>{}, grid); break;
+    case 2: f(std::integral_constant<int, 2>{}, grid); break;
+    case 4: f(std::integral_constant<int, 4>{}, grid); break;
+    case 8: f(std::integral_constant<int, 8>{}, grid); break;
+    case 16: f(std::integral_constant<int, 16>{}, grid); break;
+    case 32: f(std::integral_constant<int, 32>{}, grid); break;
+    default: f(std::integral_constant<int, 64>{}, grid); break;
   }
+  return hipGetLastError();
+}
+template <class F>
+hipError_t with_pack_narrow(int64_t rows, int32_t b, F f) {
+  const dim3 grid((unsigned)((rows + kBlock - 1) / kBlock));
+  switch (b) {
+    case 1: f(std::integral_constant<int, 1>{}, grid); break;
+    case 2: f(std::integral_constant<int, 2>{}, grid); break;
+    default: f(std::integral_constant<int, 3>{}, grid); break;
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -1756,24 +1935,28 @@ hipError_t launch_packed(const PackedArgs &p, const StreamOptions &o, hipStream_
     if (a.list_chunk[x + 1] < a.list_chunk[x]) return hipErrorInvalidValue;
     longest = std::max<int64_t>(longest, a.list_chunk[x + 1] - a.list_chunk[x]);
   }
-  const ColumnTiling t = column_tiling_max(a.b, std::max(1, std::min(o.max_lpt, kMaxLpt)));
-  const uint64_t row_bytes = (uint64_t)a.b * sizeof(float), lim = kOutOfRange;
-  const bool buf = !o.plain_loads && t.vec == 4 && row_bytes <= kMaxStride &&
-                   (uint64_t)a.A_rows * row_bytes <= lim &&
-                   (uint64_t)a.B_rows * (uint64_t)packed_pitch(a.b) <= lim &&
-                   (uint64_t)a.out_rows * row_bytes <= lim &&
-                   (uint64_t)a.n_slots * (uint64_t)a.b * sizeof(double) <= lim;
-  // Groups of at least two lanes for ragged rows, which are of 5 floats or more.
-  ColumnTiling u = t;
-  if (u.ragged && u.lpt < 2) u.lpt = 2;
-  u.width = u.lpt * u.vec;
-  u.n_slices = (a.b + u.width - 1) / u.width;
-  const void *fn = packed_fn_for(u, buf, a.weights != nullptr);
+  const bool wt = a.weights != nullptr;
+  const void *fn = nullptr;
+  int lpt = kNarrowLanes, slices = 1;
+  if (a.b <= kMaxNarrow) {
+    fn = narrow_packed_fn(a.b, wt);
+  } else {
+    // As for float rows (choose_stream); a slice begins with a scale of its own, so
+    // only rows that fit it take groups of less than kPackedLanes.
+    const uint64_t row_bytes = (uint64_t)a.b * sizeof(float), lim = kOutOfRange;
+    const bool buf = !o.plain_loads && row_bytes <= kMaxStride &&
+                     (uint64_t)a.A_rows * row_bytes <= lim &&
+                     (uint64_t)a.B_rows * (uint64_t)p.pitch <= lim &&
+                     (uint64_t)a.out_rows * row_bytes <= lim &&
+                     (uint64_t)a.n_slots * (uint64_t)a.b * sizeof(double) <= lim;
+    lpt = column_tiling_max(a.b, std::max(kPackedLanes, std::min(o.max_lpt, kMaxLpt))).lpt;
+    slices = (a.b + lpt * 4 - 1) / (lpt * 4);
+    fn = packed_fn_for(a.b % 4 != 0, lpt, buf, wt);
+  }
   if (!fn) return hipErrorInvalidValue;
-  const int64_t per_list =
-      std::max<int64_t>(1, (longest + kBlock / u.lpt - 1) / (kBlock / u.lpt));
+  const int64_t per_list = std::max<int64_t>(1, (longest + kBlock / lpt - 1) / (kBlock / lpt));
   if (per_list * a.n_lists > (int64_t)INT32_MAX) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(per_list * a.n_lists), (unsigned)u.n_slices);
+  const dim3 grid((unsigned)(per_list * a.n_lists), (unsigned)slices);
   PackedArgs arg = p;
   void *params[] = {&arg};
   if (start || stop)
@@ -1781,27 +1964,29 @@ hipError_t launch_packed(const PackedArgs &p, const StreamOptions &o, hipStream_
   return hipLaunchKernel(fn, grid, dim3(kBlock), params, 0, s);
 }
 
-hipError_t launch_pack(const float *X, int64_t rows, int32_t b, uint8_t *codes,
-                       uint8_t *exponents, hipStream_t s) {
-  return with_pack_lanes(b, [&](auto vec, auto lanes) {
-    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
-    const int64_t per = (int64_t)kBlock / L * kPackRows, blocks = (rows + per - 1) / per;
-    if (blocks * kBlock > (int64_t)UINT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((pack_kernel<V, L>), dim3((unsigned)blocks), dim3(kBlock), 0, s, X, rows, b,
-                       codes, exponents);
-    return hipGetLastError();
+hipError_t launch_pack(const float *X, int64_t rows, int32_t b, uint8_t *packed, hipStream_t s) {
+  const uint32_t pitch = (uint32_t)packed_pitch(b);
+  if (b < 4)
+    return with_pack_narrow(rows, b, [&](auto n, dim3 grid) {
+      hipLaunchKernelGGL((pack_narrow_kernel<decltype(n)::value>), grid, dim3(kBlock), 0, s, X,
+                         rows, pitch, packed);
+    });
+  return with_pack_lanes(rows, b, [&](auto lanes, dim3 grid) {
+    hipLaunchKernelGGL((pack_kernel<decltype(lanes)::value>), grid, dim3(kBlock), 0, s, X, rows, b,
+                       pitch, packed);
   });
 }
 
-hipError_t launch_unpack(const uint8_t *codes, const uint8_t *exponents, int64_t rows, int32_t b,
-                         float *X, hipStream_t s) {
-  return with_pack_lanes(b, [&](auto vec, auto lanes) {
-    constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
-    const int64_t per = (int64_t)kBlock / L * kPackRows, blocks = (rows + per - 1) / per;
-    if (blocks * kBlock > (int64_t)UINT32_MAX) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((unpack_kernel<V, L>), dim3((unsigned)blocks), dim3(kBlock), 0, s, codes,
-                       exponents, rows, b, X);
-    return hipGetLastError();
+hipError_t launch_unpack(const uint8_t *packed, int64_t rows, int32_t b, float *X, hipStream_t s) {
+  const uint32_t pitch = (uint32_t)packed_pitch(b);
+  if (b < 4)
+    return with_pack_narrow(rows, b, [&](auto n, dim3 grid) {
+      hipLaunchKernelGGL((unpack_narrow_kernel<decltype(n)::value>), grid, dim3(kBlock), 0, s,
+                         packed, rows, pitch, X);
+    });
+  return with_pack_lanes(rows, b, [&](auto lanes, dim3 grid) {
+    hipLaunchKernelGGL((unpack_kernel<decltype(lanes)::value>), grid, dim3(kBlock), 0, s, packed,
+                       rows, b, pitch, X);
   });
 }
 

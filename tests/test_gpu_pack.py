@@ -31,8 +31,8 @@ def kept(X):
     finite = np.isfinite(X)
     top = np.where(finite, np.abs(X), 0.0).max(1)
     m, k = np.frexp(top)                       # top = m 2^k, m in [1/2, 1)
-    e = np.where(top > 0, k - 9 + (m > 0.875), -127)
-    e = np.maximum(e, -127)
+    e = np.where(top > 0, k - 9 + (m > 0.875), -126)
+    e = np.maximum(e, -126)
     x = np.ldexp(np.where(finite, X, 0.0), -e[:, None])
     _, k = np.frexp(x)
     step = np.ldexp(1.0, np.maximum(k - 1, -6) - 3)
@@ -45,7 +45,7 @@ def kept(X):
 WIDTHS = [1, 2, 3, 4, 5, 6, 7, 8, 10, 31, 32, 33, 64, 93, 128, 129, 255, 256, 257, 300, 1000]
 
 
-def check_pack(kbf, X, exact_exponents=True):
+def check_pack(kbf, X):
     import torch
     P = kbf.pack(torch.from_numpy(X).cuda())
     assert P.shape == X.shape
@@ -53,8 +53,14 @@ def check_pack(kbf, X, exact_exponents=True):
     want, e = kept(X)
     assert np.array_equal(np.isnan(got), np.isnan(want))
     assert np.array_equal(got[~np.isnan(want)], want[~np.isnan(want)])
-    if exact_exponents:
-        assert np.array_equal(P.exponents.cpu().numpy().astype(np.int64), e + 127)
+    # The exponent, where a row keeps it: a byte behind the codes up to 3 values, a
+    # float before every eight dwords of them from 4 on.
+    data, b = P.data.cpu().numpy(), X.shape[1]
+    if b < 4:
+        assert np.array_equal(data[:, b].astype(np.int64), e + 127)
+    else:
+        scale = np.ascontiguousarray(data).view(np.float32)[:, ::9]
+        assert scale.shape[1] == -(-b // 32) and (scale == np.exp2(e)[:, None]).all()
     return P
 
 
@@ -215,7 +221,7 @@ def test_checked_build_counts_nothing(kbf, b):
     lib.kb_destroy.argtypes = [P]
     lib.kb_workspace_size.argtypes = [P, I32]
     lib.kb_workspace_size.restype = SZ
-    lib.kb_follow_backward_packed.argtypes = [P, I32, P, P, P, P, P, P, P, SZ, P]
+    lib.kb_follow_backward_packed.argtypes = [P, I32, P, P, P, P, P, P, SZ, P]
     lib.kb_checked_violations.argtypes = [ctypes.POINTER(ctypes.c_uint64), I32]
     s, r, o, n_e, n_r = small_kb(b)
     g = np.random.default_rng(b)
@@ -230,7 +236,7 @@ def test_checked_build_counts_nothing(kbf, b):
     ws = torch.empty(max(1, size), dtype=torch.uint8, device="cuda")
     dX, dR = torch.empty_like(X), torch.empty_like(R)
     p = lambda t: P(t.data_ptr())  # noqa: E731
-    assert lib.kb_follow_backward_packed(h, b, p(kept_.codes), p(kept_.exponents), p(R), p(dY),
+    assert lib.kb_follow_backward_packed(h, b, p(kept_.data), p(R), p(dY),
                                          p(dX), p(dR), p(ws), size,
                                          P(torch.cuda.current_stream().cuda_stream)) == 0
     torch.cuda.synchronize()
@@ -312,19 +318,17 @@ def test_captured_and_replayed(kbf):
 def test_pitch_and_c_refusals():
     import paper_2002_06115_amd as k
     lib, P = k._lib, ctypes.c_void_p
-    assert [lib.kb_packed_pitch(b) for b in (-1, 0, 1, 2, 3, 4, 5, 8, 9)] == \
-        [0, 0, 1, 2, 3, 4, 8, 8, 12]
-    x, c, e = P(1 << 20), P(1 << 21), P(1 << 22)  # never dereferenced: checked first
-    assert lib.kb_pack(0, 4, None, None, None, None) == k.KB_OK
-    for args in ((-1, 4, x, c, e), ((1 << 30) + 1, 4, x, c, e), (5, 0, x, c, e),
-                 (5, 4, None, c, e), (5, 4, x, None, e), (5, 4, x, c, None),
-                 (5, 4, P((1 << 20) + 4), c, e), (5, 5, P((1 << 20) + 2), c, e),
-                 (5, 4, x, P((1 << 21) + 2), e), (5, 4, x, P((1 << 20) + 16), e),
-                 (5, 4, x, c, P((1 << 21) + 3)), (5, 4, x, c, P((1 << 20) + 3))):
+    assert [lib.kb_packed_pitch(b) for b in (-1, 0, 1, 2, 3, 4, 5, 8, 9, 32, 33, 64, 65)] == \
+        [0, 0, 2, 4, 4, 8, 12, 12, 16, 36, 44, 72, 80]
+    x, c = P(1 << 20), P(1 << 21)  # never dereferenced: checked first
+    assert lib.kb_pack(0, 4, None, None, None) == k.KB_OK
+    for args in ((-1, 4, x, c), ((1 << 30) + 1, 4, x, c), (5, 0, x, c), (5, 4, None, c),
+                 (5, 4, x, None), (5, 4, P((1 << 20) + 4), c), (5, 5, P((1 << 20) + 2), c),
+                 (5, 4, x, P((1 << 21) + 2)), (5, 4, x, P((1 << 20) + 16))):
         assert lib.kb_pack(*args, None) == k.KB_EINVAL, args
-        rows, b, X, codes, exponents = args
-        assert lib.kb_unpack(rows, b, codes, exponents, X, None) == k.KB_EINVAL, args
-    assert lib.kb_follow_backward_packed(None, 4, c, e, x, x, x, x, None, 0, None) == k.KB_EINVAL
+        rows, b, X, packed = args
+        assert lib.kb_unpack(rows, b, packed, X, None) == k.KB_EINVAL, args
+    assert lib.kb_follow_backward_packed(None, 4, c, x, x, x, x, None, 0, None) == k.KB_EINVAL
 
 
 def test_python_refusals():
@@ -333,7 +337,7 @@ def test_python_refusals():
     with pytest.raises(TypeError):
         k.pack(torch.zeros((3, 4)))
     with pytest.raises(TypeError):
-        k.Packed(torch.zeros((3, 4), dtype=torch.uint8), torch.zeros(3, dtype=torch.uint8), 4)
+        k.Packed(torch.zeros((3, 8), dtype=torch.uint8), 4)
 
 
 @pytest.mark.gpu
@@ -348,10 +352,10 @@ def test_python_refusals_on_the_gpu(kbf):
             (ValueError, lambda: kbf.pack(X[0])),
             (ValueError, lambda: kbf.pack(X.t())),
             (ValueError, lambda: kbf.pack(X[:, :0])),
-            (TypeError, lambda: kbf.Packed(P.codes.int(), P.exponents, 5)),
-            (ValueError, lambda: kbf.Packed(P.codes, P.exponents, 9)),
-            (ValueError, lambda: kbf.Packed(P.codes, P.exponents[:5], 5)),
-            (ValueError, lambda: kbf.Packed(P.codes[:, ::2], P.exponents, 4)),
+            (TypeError, lambda: kbf.Packed(P.data.int(), 5)),
+            (ValueError, lambda: kbf.Packed(P.data, 9)),
+            (ValueError, lambda: kbf.Packed(P.data, 0)),
+            (ValueError, lambda: kbf.Packed(P.data[::2], 5)),
             (ValueError, lambda: kb.follow_backward(kbf.pack(X[:5]), R, X)),
             (ValueError, lambda: kb.follow_backward(kbf.pack(torch.zeros((6, 4), device="cuda")),
                                                     R, X)),
@@ -362,8 +366,8 @@ def test_python_refusals_on_the_gpu(kbf):
     ws = kb.workspace(5)
     at = (None, 0) if ws is None else (ws.data_ptr(), ws.numel())
     out = torch.zeros((6, 5), device="cuda")
-    go = lambda codes, dx: kbf._lib.kb_follow_backward_packed(  # noqa: E731
-        kb._handle, 5, codes, P.exponents.data_ptr(), R.data_ptr(), X.data_ptr(), dx, None, *at, None)
+    go = lambda packed, dx: kbf._lib.kb_follow_backward_packed(  # noqa: E731
+        kb._handle, 5, packed, R.data_ptr(), X.data_ptr(), dx, None, *at, None)
     assert go(None, out.data_ptr()) == kbf.KB_EINVAL
     assert go(out.data_ptr(), out.data_ptr()) == kbf.KB_EINVAL
     assert kbf.pack(X[:0]).unpack().shape == (0, 5)
