@@ -104,7 +104,7 @@ kbc_status kbc_softmax_xent_scratch(int64_t n, int32_t b, const float *z, const 
  *   table  : [rows][dim] of `type`, row r at r * stride elements (stride >= dim).
  *   out, dout, dtable : contiguous, of `type`.
  * Any element alignment will do.  1 <= rows < 2^31 - 1, tokens <= 2^30, bags <
- * 2^31 - 1, 1 <= dim <= 65536, else KBC_EINVAL.  Sums are taken in double, in a
+ * 2^31 - 1 (2^25 with mean), 1 <= dim <= 65536, else KBC_EINVAL.  Sums are taken in double, in a
  * fixed order (partial sums of 16-bit outputs in float); an output is rounded to
  * float, and to a 16-bit type from there.
  */

@@ -17,6 +17,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import torch
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("KBCHAIN_LIB", os.path.join(_HERE, "_lib", "libkbchain.so"))
 
@@ -173,20 +175,19 @@ def softmax_xent(z, t):
 
 # -- embedding lookup ----------------------------------------------------------
 
-_TYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def _type(t, name):
     """The library's code of a CUDA tensor's type."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or str(t.dtype) not in _TYPES:
+    code = _TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if code is None:
         raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA tensor")
-    return _TYPES[str(t.dtype)]
+    return code
 
 
 def _ints(t, name, device, dims, dtype=None):
     """A contiguous int32 or int64 tensor on `device`, of one of `dims` dimensions."""
-    import torch
     if not isinstance(t, torch.Tensor) or t.dtype not in (torch.int32, torch.int64) or \
             t.device != device:
         raise TypeError(f"{name} must be an int32 or int64 tensor on {device}")
@@ -199,9 +200,9 @@ def _ints(t, name, device, dims, dtype=None):
 
 def _run(fn, what, device, *args):
     """fn(*args, stream) on the current stream of `device`, with that device current."""
-    import torch
-    stream = torch._C._cuda_getCurrentRawStream(device.index)
-    if torch.cuda.current_device() == device.index:
+    index = device.index
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if torch._C._cuda_getDevice() == index:
         status = fn(*args, stream)
     else:
         with torch.cuda.device(device):
@@ -212,7 +213,6 @@ def _run(fn, what, device, *args):
 def _bytes(n, device):
     """(tensor, address, bytes) of n bytes of scratch; the tensor is held until
     the call is enqueued."""
-    import torch
     if n == 0:
         return None, None, 0
     s = torch.empty(n, dtype=torch.uint8, device=device)
@@ -238,7 +238,6 @@ def _bag_args(ids, offsets, pool, device):
 
 
 def _embed_forward(table, ids, offsets, scale, pool):
-    import torch
     code = _type(table, "table")
     if table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 1:
         raise ValueError("table must be [rows][dim], not empty")
@@ -266,7 +265,6 @@ def _embed_forward(table, ids, offsets, scale, pool):
 def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
     """The gradient [rows][dim] of embed's table, of dout's type, for the upstream
     gradient dout of its output; rows that no id names are zeros."""
-    import torch
     code = _type(dout, "dout")
     device = dout.device
     bags, at = _bag_args(ids, offsets, pool, device)
@@ -286,59 +284,20 @@ def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
     return dtable
 
 
-_functions = {}
+class _Embed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, offsets, scale, pool):
+        ctx.save_for_backward(ids, offsets)
+        ctx.args = table.shape[0], table.dtype, scale, pool
+        return _embed_forward(table, ids, offsets, scale, pool)
 
-
-def _function(name):
-    """The autograd function of an operation of this module (torch is imported
-    where it is needed)."""
-    if name not in _functions:
-        _functions.update(_make_functions())
-    return _functions[name]
-
-
-def _make_functions():
-    import torch
-
-    class Embed(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, table, ids, offsets, scale, pool):
-            ctx.save_for_backward(ids, offsets)
-            ctx.args = table.shape[0], table.dtype, scale, pool
-            return _embed_forward(table, ids, offsets, scale, pool)
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, dout):
-            ids, offsets = ctx.saved_tensors
-            rows, dtype, scale, pool = ctx.args
-            return (embed_backward(dout.to(dtype).contiguous(), ids, rows, offsets, scale, pool),
-                    None, None, None, None)
-
-    class Constrain(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
-            out = _constrain_forward(z, bias, allowed, history, offsets, repeat, presence,
-                                     frequency, fill)
-            each = isinstance(repeat, torch.Tensor)
-            scaled = history is not None and (each or repeat != 1.0)
-            ctx.save_for_backward(z if scaled else None, allowed, history if scaled else None,
-                                  offsets, repeat if each else None)
-            ctx.args = z.dtype, None if each else repeat, None if bias is None else bias.dim()
-            return out
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, dout):
-            z, allowed, history, offsets, repeat = ctx.saved_tensors
-            dtype, repeat_all, bias_dims = ctx.args
-            dz, dbias = constrain_backward(
-                dout.contiguous(), z, allowed, history, None if history is None else offsets,
-                repeat_all if repeat is None else repeat,
-                bias_dims if ctx.needs_input_grad[1] else None, dtype)
-            return dz, dbias, None, None, None, None, None, None, None
-
-    return {"embed": Embed, "constrain": Constrain}
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        ids, offsets = ctx.saved_tensors
+        rows, dtype, scale, pool = ctx.args
+        return (embed_backward(dout.to(dtype).contiguous(), ids, rows, offsets, scale, pool),
+                None, None, None, None)
 
 
 def embed(table, ids, offsets=None, scale=1.0, pool=None):
@@ -351,9 +310,8 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     padding: zeros, no term, not counted by the mean, no gradient; a bag of nothing
     else is zeros.  Differentiable with respect to table.
     """
-    import torch
     if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
-        return _function("embed").apply(table, ids, offsets, scale, pool)
+        return _Embed.apply(table, ids, offsets, scale, pool)
     return _embed_forward(table, ids, offsets, scale, pool)
 
 
@@ -361,7 +319,6 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
 
 def _limits(n, b, device, bias, allowed, history, offsets, penalties):
     """The library's description of what is asked of [n][b] logits on `device`."""
-    import torch
     l = _Limits(repeat_all=1.0)
     if bias is not None:
         if not isinstance(bias, torch.Tensor) or bias.dtype != torch.float32 or \
@@ -411,7 +368,6 @@ def _logits(z, name):
 
 
 def _constrain_forward(z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
-    import torch
     n, b, code = _logits(z, "z")
     l = _limits(n, b, z.device, bias, allowed, history, offsets,
                 {"repeat": repeat, "presence": presence, "frequency": frequency})
@@ -419,6 +375,30 @@ def _constrain_forward(z, bias, allowed, history, offsets, repeat, presence, fre
     _run(_lib.kbc_constrain, "kbc_constrain", z.device, n, b, z.data_ptr(), code, l, float(fill),
          out.data_ptr())
     return out
+
+
+class _Constrain(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
+        out = _constrain_forward(z, bias, allowed, history, offsets, repeat, presence,
+                                 frequency, fill)
+        each = isinstance(repeat, torch.Tensor)
+        scaled = history is not None and (each or repeat != 1.0)
+        ctx.save_for_backward(z if scaled else None, allowed, history if scaled else None,
+                              offsets, repeat if each else None)
+        ctx.args = z.dtype, None if each else repeat, None if bias is None else bias.dim()
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        z, allowed, history, offsets, repeat = ctx.saved_tensors
+        dtype, repeat_all, bias_dims = ctx.args
+        dz, dbias = constrain_backward(
+            dout.contiguous(), z, allowed, history, None if history is None else offsets,
+            repeat_all if repeat is None else repeat,
+            bias_dims if ctx.needs_input_grad[1] else None, dtype)
+        return dz, dbias, None, None, None, None, None, None, None
 
 
 def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0, presence=0.0,
@@ -439,11 +419,10 @@ def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0
     equal parts where it is finite; chain.softmax_xent wants a finite fill.
     Differentiable with respect to z and bias.
     """
-    import torch
     args = (z, bias, allowed, history, offsets, repeat, presence, frequency, fill)
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
                                        for t in (z, bias)):
-        return _function("constrain").apply(*args)
+        return _Constrain.apply(*args)
     return _constrain_forward(*args)
 
 
@@ -452,7 +431,6 @@ def constrain_backward(dout, z=None, allowed=None, history=None, offsets=None, r
     """(dz, dbias) of constrain for the upstream gradient dout [n][b]: dz of z's type
     (dtype's where z is not given; z is needed where a history has a repeat), dbias
     None, or with bias_dims 1 or 2 that of a bias [n] or [n][b]."""
-    import torch
     dout = _mat(dout, "dout")
     device = dout.device
     n, b = dout.shape

@@ -301,7 +301,7 @@ void with_type(kbc_type type, F f) {
 
 bool bad_limits(int64_t n, int32_t b, kbc_type type, const kbc_limits *l) {
   if (n < 1 || n > kMostRows || b < 1 || bad_type(type) || !l) return true;
-  if (ceil_div(n * b, kMostTile) > kMostBlocks || ceil_div(n, 4) > kMostBlocks) return true;
+  if (ceil_div(n * b, kMostTile) > kMostBlocks) return true;
   if (l->entries < 0 || l->entries > kMostTokens) return true;
   if (l->entries > 0) {
     if (!l->history || (l->id_bytes != 4 && l->id_bytes != 8)) return true;
@@ -340,10 +340,26 @@ void launch_dense(const Args &a, hipStream_t s) {
                        dim3(kThreads), 0, s, a);
 }
 
-template <class T, int G>
+// Lanes of a row in row_kernel: 4 elements each, or 4 at a time.
+int row_lanes(int32_t b) {
+  int lanes = 2;
+  while (lanes * 4 < b && lanes < kWave) lanes <<= 1;
+  return lanes;
+}
+
+template <class T>
 void launch_rows(const Args &a, hipStream_t s) {
-  hipLaunchKernelGGL((row_kernel<T, G>), dim3((unsigned)ceil_div(a.n, kThreads / G)),
-                     dim3(kThreads), 0, s, a);
+  const int lanes = row_lanes(a.b);
+  const dim3 grid((unsigned)ceil_div(a.n, kThreads / lanes));
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a); };
+  switch (lanes) {
+    case 2: go(row_kernel<T, 2>); break;
+    case 4: go(row_kernel<T, 4>); break;
+    case 8: go(row_kernel<T, 8>); break;
+    case 16: go(row_kernel<T, 16>); break;
+    case 32: go(row_kernel<T, 32>); break;
+    default: go(row_kernel<T, 64>); break;
+  }
 }
 
 }  // namespace
@@ -377,6 +393,8 @@ kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type 
   if (bad_limits(n, b, type, l) || !dout || !dz) return KBC_EINVAL;
   const bool scaled = l->entries > 0 && (l->repeat || l->repeat_all != 1.0f);
   if (scaled && !z) return KBC_EINVAL;
+  const bool shared = dbias && !l->bias_each;
+  if (shared && ceil_div(n, kThreads / row_lanes(b)) > kMostBlocks) return KBC_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Args a = args_for(n, b, l);
   a.z = z;
@@ -385,19 +403,8 @@ kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type 
   a.dbias = dbias;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    if (dbias && !l->bias_each) {
-      if (b <= 8)
-        launch_rows<T, 2>(a, s);
-      else if (b <= 16)
-        launch_rows<T, 4>(a, s);
-      else if (b <= 32)
-        launch_rows<T, 8>(a, s);
-      else if (b <= 64)
-        launch_rows<T, 16>(a, s);
-      else if (b <= 128)
-        launch_rows<T, 32>(a, s);
-      else
-        launch_rows<T, 64>(a, s);
+    if (shared) {
+      launch_rows<T>(a, s);
     } else {
       launch_dense<T, true>(a, s);
     }

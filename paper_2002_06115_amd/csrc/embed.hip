@@ -808,6 +808,10 @@ dim3 list_grid(ListArgs *a, int64_t list_wgs, int k, int launches) {
   return dim3((unsigned)(list_wgs + a->weight_wgs + to - from));
 }
 
+// Whether the workgroups that weigh bags fit a grid beside the others.
+bool too_many_bags(int64_t bags, int32_t mean) {
+  return mean && bags >= int64_t(1) << 25;
+}
 bool bad_sizes(int64_t tokens, int64_t bags, int64_t rows, int32_t dim, int32_t id_bytes) {
   return tokens < 0 || tokens > kMostTokens || bags < 0 || bags > kMostRows || rows < 1 ||
          rows > kMostRows || dim < 1 || dim > 65536 || (id_bytes != 4 && id_bytes != 8);
@@ -871,6 +875,7 @@ kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int
   }
   const int lpg = group_lanes(type, dim);
   const Scratch at = scratch_for(tokens, bags, dim, false, mean != 0, lpg);
+  if (too_many_bags(bags, mean)) return KBC_EINVAL;
   if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
   char *w = static_cast<char *>(scratch);
   ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, reinterpret_cast<double *>(w + at.weights),
@@ -900,6 +905,7 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
   if (tokens > 0 && (!ids || !dout)) return KBC_EINVAL;
   const int lpg = group_lanes(type, dim);
   mean = mean && bags > 0;
+  if (too_many_bags(bags, mean)) return KBC_EINVAL;
   const Scratch at = scratch_for(tokens, bags, dim, true, mean != 0, lpg);
   if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -821,8 +821,13 @@ __global__ __launch_bounds__(kBlock) void narrow_kernel(StreamArgs a) {
 // from floats.  Decoding is exact (4 significant bits, within a float's range): dR is
 // the sum over the kept values with one rounding, as from a float X.
 //
-// A scale in an array of its own would be one more line per run start (10 M entities,
-// b = 32, dR 969 us; float X 757).
+// Bound like the stream kernel by its requests, a line or two each, whose bytes are
+// fewer: dR of the training-shaped KB at b = 256 2112 us (float X 2558), of 12.9 M
+// entities and 43.7 M triples at b = 10 720 (815), of 1 M entities and 8 M weighted
+// triples at b = 64 220 (246).  A row of b = 32 is 36 bytes, of which every fourth
+// crosses a line, where a float row is a line: 10 M entities, 50 M triples 806 (754; 748
+// with rows padded to 64 bytes, which would nearly double what is kept).  With the
+// scale in an array of its own, one line more per run start, it took 969.
 //
 // LANE: 4 floats per lane, or kRaggedLane likewise.
 

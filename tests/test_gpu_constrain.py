@@ -383,3 +383,53 @@ def test_python_refusals_on_the_gpu(chain):
             (TypeError, lambda: chain.constrain_backward(z.half()))]:
         with pytest.raises(error):
             call()
+
+
+@pytest.mark.gpu
+def test_large_offsets(chain):
+    """More than 2^31 elements."""
+    import torch
+    n, b = 33_600_000, 65
+    z = torch.zeros((n, b), dtype=torch.bfloat16, device="cuda")
+    z[-1, -1], z[-1, 0] = 2.0, -2.0
+    history = torch.full((b, 1), n - 1, device="cuda")
+    allowed = torch.ones(n, dtype=torch.bool, device="cuda")
+    allowed[-2] = False
+    out = chain.constrain(z, allowed=allowed, history=history, repeat=4.0, fill=-9.0)
+    assert float(out[-1, -1]) == 0.5 and float(out[-1, 0]) == -8.0
+    assert (out[-2] == -9.0).all() and not out[:-2].any()
+    dz, db = chain.constrain_backward(out, z, allowed, history, repeat=4.0, bias_dims=1)
+    assert float(dz[-1, -1]) == 0.125 and float(dz[-1, 0]) == -32.0 and not dz[:-1].any()
+    assert float(db[-1]) == -7.5 and not db[:-1].any()
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once(chain):
+    """Calls of both operators on two streams, their tensors made on a third."""
+    import torch
+    g = np.random.default_rng(21)
+    table = torch.from_numpy(g.standard_normal((3000, 64)).astype(np.float32)).cuda()
+    sets = []
+    for k in range(2):
+        ids = torch.from_numpy(g.integers(-1, 3000, (40, 300))).cuda()
+        z = torch.from_numpy(g.standard_normal((4000, 40)).astype(np.float32)).cuda()
+        sets.append((ids, z, torch.cuda.Stream()))
+
+    def step(ids, z):
+        q = chain.embed(table, ids, pool="mean")
+        out = chain.constrain(z, history=ids, repeat=1.5, frequency=0.1)
+        return (q, chain.embed_backward(q, ids, 3000, pool="mean"), out,
+                chain.constrain_backward(out, z, None, ids, None, 1.5, 1)[1])
+
+    want = [step(ids, z) for ids, z, _ in sets]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for ids, z, stream in sets:
+            stream.wait_stream(torch.cuda.default_stream())
+            with torch.cuda.stream(stream):
+                got.append(step(ids, z))
+    torch.cuda.synchronize()
+    for k, outs in enumerate(got):
+        for x, y in zip(outs, want[k % 2]):
+            assert torch.equal(x, y)
