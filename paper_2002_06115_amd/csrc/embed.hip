@@ -57,6 +57,15 @@ __device__ __forceinline__ void load_vals(const T *p, T (&v)[VEC]) {
   }
 }
 
+// x rounded to float, and from there to T.  The compiler would otherwise make one
+// conversion of the two, 40 instructions long.
+template <class T>
+__device__ __forceinline__ T round_to(double x) {
+  float f = (float)x;
+  if constexpr (sizeof(T) == 2) asm("" : "+v"(f));
+  return (T)f;
+}
+
 // Output rows are written once and not read again by these kernels.
 template <class T, int VEC>
 __device__ __forceinline__ void store_vals(T *p, const T (&v)[VEC]) {
@@ -177,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void pool_kernel(PoolArgs a) {
   const double w = (double)a.scale / (a.mean && count > 0 ? (double)count : 1.0);
   T y[VEC];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) y[i] = (T)(float)(acc[i] * w);
+  for (int i = 0; i < VEC; ++i) y[i] = round_to<T>(acc[i] * w);
   store_vals<T, VEC>(static_cast<T *>(a.out) + g * a.dim + c, y);
 }
 
@@ -532,7 +541,7 @@ __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c,
   const double w = a.out_weights ? a.scale * a.out_weights[key] : a.scale;
   T y[VEC];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) y[i] = (T)(float)(acc[i] * w);
+  for (int i = 0; i < VEC; ++i) y[i] = round_to<T>(acc[i] * w);
   store_vals<T, VEC>(static_cast<T *>(a.out) + (int64_t)key * a.dim + c, y);
 }
 
