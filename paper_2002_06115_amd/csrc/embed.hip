@@ -735,13 +735,13 @@ void with_rows(kbc_type type, int32_t dim, F f) {
   }
 }
 
-// Entries of a chunk: about 4096 waves' worth of lane groups over the list, at
-// least kSumRows entries each (262144 tokens of 512 float16 values: gradient 154 us;
-// with 2048 waves 183, with 8192 164, which leave too little in flight or too many
-// partial sums).
+// Entries of a chunk: about 2048 waves' worth of lane groups over the list, at
+// least kSumRows entries each (gradient of 16389 tokens of 1001 bfloat16 values and of
+// 262144 of 512 float16: with 2048 waves 71 and 112 us, with 4096 77 and 112, with
+// 8192, and so more partial sums, 77 and 127).
 int32_t chunk_for(int64_t tokens, int lpg) {
   int32_t chunk = kSumRows;
-  while (chunk < 128 && tokens * lpg > (int64_t)chunk * 4096 * kWave) chunk *= 2;
+  while (chunk < 128 && tokens * lpg > (int64_t)chunk * 2048 * kWave) chunk *= 2;
   return chunk;
 }
 
