@@ -63,6 +63,112 @@ __device__ __forceinline__ float bias_of(const Args &a, int64_t i, int32_t col) 
   return a.bias ? a.bias[a.bias_each ? i * a.b + col : i] : 0.0f;
 }
 
+// M <= 4 neighbours of the arrays: the place, row and column of the first.
+struct Four {
+  int64_t f, i;
+  int32_t col;
+  int m;
+};
+__device__ __forceinline__ bool one_row(const Args &a, const Four &p) {
+  return p.m == 4 && p.col + 4 <= a.b;
+}
+// idx(row, column) of each of the four, the first's again where there are less.
+template <class F>
+__device__ __forceinline__ void places(const Args &a, const Four &p, F idx, int64_t (&at)[4]) {
+  int64_t i = p.i;
+  int32_t col = p.col;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    at[e] = e < p.m ? idx(i, col) : idx(p.i, p.col);
+    if (++col == a.b) {
+      col = 0;
+      ++i;
+    }
+  }
+}
+// Bit e: whether the e-th of them is allowed.
+__device__ __forceinline__ unsigned allowed4(const Args &a, const Four &p) {
+  if (a.allowed_kind == kAll) return 15;
+  if (a.allowed_kind == kBytes) {
+    const uint8_t *w = static_cast<const uint8_t *>(a.allowed);
+    if (!a.allowed_each && one_row(a, p)) return w[p.i] ? 15 : 0;
+    uchar4_any t;
+    if (a.allowed_each && p.m == 4) {
+      t = *reinterpret_cast<const uchar4_any *>(w + p.f);
+    } else {
+      int64_t at[4];
+      places(a, p, [&](int64_t i, int32_t col) { return a.allowed_each ? i * a.b + col : i; }, at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = w[at[e]];
+    }
+    return (t[0] ? 1 : 0) | (t[1] ? 2 : 0) | (t[2] ? 4 : 0) | (t[3] ? 8 : 0);
+  }
+  const uint32_t *w = static_cast<const uint32_t *>(a.allowed);
+  if (one_row(a, p)) {
+    const int bit = (int)(p.i & 31);
+    if (!a.allowed_each) return w[p.i >> 5] >> bit & 1 ? 15 : 0;
+    const vec4_any<uint32_t> t =
+        *reinterpret_cast<const vec4_any<uint32_t> *>(w + (p.i >> 5) * a.b + p.col);
+    return (t[0] >> bit & 1) | (t[1] >> bit & 1) << 1 | (t[2] >> bit & 1) << 2 |
+           (t[3] >> bit & 1) << 3;
+  }
+  int64_t at[4], row[4];
+  places(a, p, [&](int64_t i, int32_t col) { return a.allowed_each ? (i >> 5) * a.b + col : i >> 5; },
+         at);
+  places(a, p, [&](int64_t i, int32_t) { return i; }, row);
+  uint32_t t[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) t[e] = w[at[e]];
+  unsigned ok = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ok |= (t[e] >> (row[e] & 31) & 1) << e;
+  return ok;
+}
+__device__ __forceinline__ void bias4(const Args &a, const Four &p, float (&v)[4]) {
+  if (!a.bias) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = 0.0f;
+  } else if (a.bias_each && p.m == 4) {
+    const float4_any t = *reinterpret_cast<const float4_any *>(a.bias + p.f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = t[e];
+  } else if (!a.bias_each && one_row(a, p)) {
+    const float t = a.bias[p.i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = t;
+  } else {
+    int64_t at[4];
+    places(a, p, [&](int64_t i, int32_t col) { return a.bias_each ? i * a.b + col : i; }, at);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a.bias[at[e]];
+  }
+}
+// The first m <= 4 values at p (zeros for the others), and the way back.
+template <class T>
+__device__ __forceinline__ vec4_any<T> load4(const T *p, int m) {
+  vec4_any<T> v;
+  if (m == 4) {
+    v = *reinterpret_cast<const vec4_any<T> *>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = e < m ? p[e] : (T)0.0f;
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void store4(T *p, int m, const float (&y)[4]) {
+  if (m == 4) {
+    vec4_any<T> v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (T)y[e];
+    __builtin_nontemporal_store(v, reinterpret_cast<vec4_any<T> *>(p));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < m) p[e] = (T)y[e];
+  }
+}
+
 // -- every element, as if no history were ---------------------------------------------
 
 // Vectors of 4 elements of a thread, and elements of a workgroup: DEPTH 1 where an
@@ -82,97 +188,59 @@ __global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
   const int64_t row0 = first / a.b;
   const uint32_t rest = (uint32_t)(first - row0 * a.b);
   vec4_any<In> v[DEPTH];
-#pragma unroll
-  for (int k = 0; k < DEPTH; ++k) {
-    const int64_t f = first + (k * kThreads + (int)threadIdx.x) * 4;
-    if (f + 4 <= size) {
-      v[k] = *reinterpret_cast<const vec4_any<In> *>(in + f);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[k][e] = f + e < size ? in[f + e] : (In)0.0f;
-    }
-  }
+  Four p[DEPTH];
 #pragma unroll
   for (int k = 0; k < DEPTH; ++k) {
     const uint32_t local = (uint32_t)(k * kThreads + (int)threadIdx.x) * 4;
-    const int64_t f = first + local;
-    if (f >= size) break;
     // The row and column of the first of the four: exact, as the dividend is
     // below 2 b where b is above kMostTile, and below 2 kMostTile where it is not.
     const uint32_t x = rest + local;
-    const uint32_t q = a.b > kMostTile ? (uint32_t)(x >= (uint32_t)a.b) : a.b == 1 ? x : __umulhi(x, a.magic);
-    int64_t i = row0 + q;
-    int32_t col = (int32_t)(x - q * (uint32_t)a.b);
+    const uint32_t q = a.b > kMostTile ? (uint32_t)(x >= (uint32_t)a.b)
+                       : a.b == 1      ? x
+                                       : __umulhi(x, a.magic);
+    p[k] = {first + local, row0 + q, (int32_t)(x - q * (uint32_t)a.b),
+            (int)max((int64_t)0, min((int64_t)4, size - first - local))};
+    v[k] = load4<In>(in + p[k].f, p[k].m);
+  }
+#pragma unroll
+  for (int k = 0; k < DEPTH; ++k) {
+    if (p[k].m == 0) break;
+    const unsigned ok = allowed4(a, p[k]);
     float y[4];
-    bool ok[4];
+    if constexpr (BACKWARD) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool in_range = f + e < size;
-      ok[e] = in_range && is_allowed(a, i, col);
-      y[e] = (float)v[k][e];
-      if constexpr (BACKWARD) {
-        y[e] = ok[e] ? y[e] : 0.0f;
-      } else {
-        if (in_range) y[e] += bias_of(a, i, col);
-        y[e] = ok[e] ? y[e] : a.fill;
-      }
-      if (++col == a.b) {
-        col = 0;
-        ++i;
-      }
-    }
-    if (f + 4 <= size) {
-      vec4_any<Out> o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (Out)y[e];
-      __builtin_nontemporal_store(o, reinterpret_cast<vec4_any<Out> *>(out + f));
+      for (int e = 0; e < 4; ++e) y[e] = ok >> e & 1 ? (float)v[k][e] : 0.0f;
     } else {
+      bias4(a, p[k], y);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (f + e < size) out[f + e] = (Out)y[e];
+      for (int e = 0; e < 4; ++e) y[e] = ok >> e & 1 ? (float)v[k][e] + y[e] : a.fill;
     }
+    store4<Out>(out + p[k].f, p[k].m, y);
     if constexpr (BACKWARD)
-      if (a.dbias) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (f + e < size) a.dbias[f + e] = y[e];
-      }
+      if (a.dbias) store4<float>(a.dbias + p[k].f, p[k].m, y);
   }
 }
 
-// The backward pass with a shared bias: G lanes a row, which they also sum.
+// The backward pass with a shared bias: G lanes a row, which they also sum.  (Four
+// rows of a group in flight took as long for 64 million elements, and 16.8 us for
+// 14.8 for 4 million, with the history's launch.)
 template <class T, int G>
 __global__ __launch_bounds__(kThreads) void row_kernel(Args a) {
   const int lane = threadIdx.x % G;
   const int64_t i = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
   if (i >= a.n) return;  // whole groups; their shuffles stay inside the group
-  const float *g = a.dout + i * a.b;
-  T *dz = static_cast<T *>(a.out) + i * a.b;
   double sum = 0.0;
   for (int64_t c = lane * 4; c < a.b; c += G * 4) {
-    const int m = (int)min((int64_t)4, a.b - c);
-    float v[4];
-    if (m == 4) {
-      const float4_any t = *reinterpret_cast<const float4_any *>(g + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = t[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < m ? g[c + e] : 0.0f;
-    }
+    const Four p = {i * a.b + c, i, (int32_t)c, (int)min((int64_t)4, a.b - c)};
+    const vec4_any<float> v = load4<float>(a.dout + p.f, p.m);
+    const unsigned ok = allowed4(a, p);
+    float y[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[e] = e < m && is_allowed(a, i, (int32_t)(c + e)) ? v[e] : 0.0f;
-      sum += (double)v[e];
+      y[e] = ok >> e & 1 ? v[e] : 0.0f;  // (those past the row are zeros)
+      sum += (double)y[e];
     }
-    if (m == 4) {
-      vec4_any<T> o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = (T)v[e];
-      __builtin_nontemporal_store(o, reinterpret_cast<vec4_any<T> *>(dz + c));
-    } else {
-      for (int e = 0; e < m; ++e) dz[c + e] = (T)v[e];
-    }
+    store4<T>(static_cast<T *>(a.out) + p.f, p.m, y);
   }
 #pragma unroll
   for (int m = 1; m < G; m <<= 1) sum += __shfl_xor(sum, m);
@@ -285,9 +353,9 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
 
 // -- how a call is launched ----------------------------------------------------------------
 
-// Elements from which workgroups take 4 vectors a thread: 4 million of 43000 rows
-// of 93 columns take 13.2 us with one vector and 14.5 with four (with the history's
-// launch), 64 million 92 to 100 and 97 to 100.
+// Elements from which workgroups take 4 vectors a thread: 64 million take 81 us with
+// four and 90 with one; 4 million of 43000 rows of 93 columns, with the history's
+// launch, 15.8 and 12.9.
 constexpr int64_t kSmall = 1 << 22;
 
 template <class F>
