@@ -11,9 +11,10 @@
 // takes its last 16 bytes again), several rows in flight.  A pooled sum over few
 // tokens is one workgroup a bag.  The gradient, and pooled sums over many
 // tokens, are one segmented sum: a list of (row of the output, row read), sorted
-// by the first, is cut into equal chunks, one a lane group, that are walked in
-// order; a row that lies inside its chunk is written at once, a row that crosses
-// chunks leaves one partial sum per chunk, added in order by the second launch.
+// by the first, is cut into equal chunks, one a workgroup, and those into runs, one
+// a lane group, that are walked in order.  A row that lies inside its run is written
+// at once, one inside its chunk after the groups have met in LDS, and one that
+// crosses chunks leaves one partial sum per chunk, added in order by the next launch.
 // So the work is spread evenly however often a word occurs, nothing is atomic,
 // and two calls give the same bits.  Sums are taken in double (see Slot); an output is
 // rounded to float and, in a 16-bit type, from there to the type.
@@ -222,12 +223,17 @@ __device__ __forceinline__ int2 grad_entry(const ListArgs &a, int key, int64_t t
 
 // 1 / tokens of four bags, a wave each; a long one by the whole workgroup.
 constexpr int64_t kLongBag = 4096;
+constexpr int kCountLoads = 8;  // in flight
 __device__ __forceinline__ int count_ids(const ListArgs &a, int64_t begin, int64_t end, int lane,
                                          int lanes) {
   int n = 0;
-  for (int64_t t = begin + lane; t < end; t += lanes) {
-    const int64_t id = load_int(a.ids, t);
-    n += id >= 0 && id < a.rows;
+  for (int64_t t = begin + lane; t < end; t += lanes * kCountLoads) {
+    int64_t id[kCountLoads];
+#pragma unroll
+    for (int u = 0; u < kCountLoads; ++u) id[u] = load_int(a.ids, min(t + u * lanes, end - 1));
+#pragma unroll
+    for (int u = 0; u < kCountLoads; ++u)
+      n += t + u * lanes < end && id[u] >= 0 && id[u] < a.rows;
   }
   for (int m = 1; m < kWave; m <<= 1) n += __shfl_xor(n, m);
   return n;
@@ -514,7 +520,8 @@ __global__ __launch_bounds__(kThreads) void radix_place_kernel(RadixArgs a) {
 struct SumArgs {
   const int2 *entries;
   int64_t n;
-  int32_t chunk;
+  int32_t run;    // entries of a lane group
+  int32_t chunk;  // of a workgroup
   const void *src;
   int64_t src_stride;
   int32_t dim;
@@ -524,7 +531,7 @@ struct SumArgs {
   void *out;
   int64_t out_rows;
   void *slots;  // Slot<type> [chunk][2][dim]: the sum of the chunk's first row, if it began
-                // before the chunk, and of its last one, if that goes on behind it
+                // before the chunk, and of its last one, if it began in it and goes on
 };
 // Partial sums of a row: double, and float where the row is rounded to 16 bits in the
 // end, 2^-24 of them against its 2^-9 or 2^-12 (half the bytes, a tenth of all that
@@ -548,65 +555,104 @@ __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c,
 template <class T, int VEC, int LPG>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   constexpr int GPB = kThreads / LPG;
-  const int lane = threadIdx.x % LPG;
-  const int64_t q = (int64_t)blockIdx.x * GPB + threadIdx.x / LPG;
+  // Of each lane group: the sum of its first row, if that began before its entries,
+  // and whether it goes on behind them.
+  __shared__ Slot<T> head[GPB][LPG * VEC];
+  __shared__ int goes_on[GPB];
+  const int lane = threadIdx.x % LPG, grp = threadIdx.x / LPG;
   const int c0 = blockIdx.y * (LPG * VEC) + lane * VEC;
-  const int64_t p0 = q * a.chunk, p1 = min(a.n, p0 + a.chunk);
-  if (p0 >= a.n || c0 >= a.dim) return;  // no barrier below
-  const int c = min(c0, a.dim - VEC);
+  const int64_t p0 = (int64_t)blockIdx.x * a.chunk + (int64_t)grp * a.run;
+  const int64_t p1 = min(a.n, p0 + a.run);
+  const bool active = c0 < a.dim;
+  const int c = active ? min(c0, a.dim - VEC) : 0;
   const T *src = static_cast<const T *>(a.src);
-  int key = a.entries[p0].x;
-  bool began = p0 == 0 || a.entries[p0 - 1].x != key;  // the current row began in this chunk
   double acc[VEC];
+  int key = -1;
+  bool late = false;  // the group's first row began before its entries
+  bool open = false;  // its last row began in them and goes on: acc is its sum so far
+  auto put = [&]() {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+    for (int i = 0; i < VEC; ++i) head[grp][lane * VEC + i] = (Slot<T>)acc[i];
+  };
+  if (active && p0 < a.n) {
+    key = a.entries[p0].x;
+    late = p0 > 0 && a.entries[p0 - 1].x == key;
+    bool began = !late;  // the current row began in these entries
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+    int2 next[kSumRows];  // the entries of the next rows are read while these arrive
+#pragma unroll
+    for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p0 + k, p1 - 1)];
+    for (int64_t p = p0; p < p1; p += kSumRows) {
+      int2 e[kSumRows];
+      T v[kSumRows][VEC];
+      double w[kSumRows];
+#pragma unroll
+      for (int k = 0; k < kSumRows; ++k) e[k] = next[k];
+#pragma unroll
+      for (int k = 0; k < kSumRows; ++k) {
+        const int r = max(e[k].y, 0);
+        load_vals<T, VEC>(src + (int64_t)r * a.src_stride + c, v[k]);
+        w[k] = a.src_weights ? a.src_weights[r] : 1.0;
+      }
+#pragma unroll
+      for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p + kSumRows + k, p1 - 1)];
+#pragma unroll
+      for (int k = 0; k < kSumRows; ++k) {
+        if (p + k >= p1) break;
+        if (e[k].x != key) {
+          if (began)
+            write_row<T, VEC>(a, key, c, acc);
+          else
+            put();
+          began = true;
+          key = e[k].x;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+        }
+        if (e[k].y >= 0) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) acc[i] += (double)(float)v[k][i] * w[k];
+        }
+      }
+    }
+    const bool more = p1 < a.n && a.entries[p1].x == key;
+    if (!began)
+      put();
+    else if (more)
+      open = true;
+    else
+      write_row<T, VEC>(a, key, c, acc);
+    if (late) goes_on[grp] = !began && more;
+  }
+  __syncthreads();
+  // Rows that go on in the workgroup's next groups: the group where one began adds
+  // theirs in order; what crosses the workgroup's ends goes to its slots.
+  auto add_heads = [&](int k) {  // of groups k on; whether the row goes on behind all
+    for (; k < GPB; ++k) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) acc[i] += (double)head[k][lane * VEC + i];
+      if (!goes_on[k]) return false;
+    }
+    return true;
+  };
   auto slot = [&](int which) {
-    Slot<T> *s = static_cast<Slot<T> *>(a.slots) + (q * 2 + which) * a.dim + c;
+    Slot<T> *s = static_cast<Slot<T> *>(a.slots) + ((int64_t)blockIdx.x * 2 + which) * a.dim + c;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) s[i] = (Slot<T>)acc[i];
   };
-  int2 next[kSumRows];  // the entries of the next rows are read while these arrive
-#pragma unroll
-  for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p0 + k, p1 - 1)];
-  for (int64_t p = p0; p < p1; p += kSumRows) {
-    int2 e[kSumRows];
-    T v[kSumRows][VEC];
-    double w[kSumRows];
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k) e[k] = next[k];
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k) {
-      const int r = max(e[k].y, 0);
-      load_vals<T, VEC>(src + (int64_t)r * a.src_stride + c, v[k]);
-      w[k] = a.src_weights ? a.src_weights[r] : 1.0;
-    }
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k) next[k] = a.entries[min(p + kSumRows + k, p1 - 1)];
-#pragma unroll
-    for (int k = 0; k < kSumRows; ++k) {
-      if (p + k >= p1) break;
-      if (e[k].x != key) {
-        if (began)
-          write_row<T, VEC>(a, key, c, acc);
-        else
-          slot(0);
-        began = true;
-        key = e[k].x;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
-      }
-      if (e[k].y >= 0) {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) acc[i] += (double)(float)v[k][i] * w[k];
-      }
-    }
+  if (open) {
+    if (add_heads(grp + 1))
+      slot(1);
+    else
+      write_row<T, VEC>(a, key, c, acc);
   }
-  if (p1 < a.n && a.entries[p1].x == key)
-    slot(began ? 1 : 0);
-  else if (began)
-    write_row<T, VEC>(a, key, c, acc);
-  else
+  if (grp == 0 && late) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] = 0.0;
+    (void)add_heads(0);
     slot(0);
+  }
 }
 
 // Rows that cross chunks: the wave of the chunk where the row began adds its partial
@@ -735,15 +781,16 @@ void with_rows(kbc_type type, int32_t dim, F f) {
   }
 }
 
-// Entries of a chunk: about 2048 waves' worth of lane groups over the list, at
-// least kSumRows entries each (gradient of 16389 tokens of 1001 bfloat16 values and of
+// Entries of a lane group: about 2048 waves' worth of groups over the list, at least
+// kSumRows entries each (gradient of 16389 tokens of 1001 bfloat16 values and of
 // 262144 of 512 float16: with 2048 waves 71 and 112 us, with 4096 77 and 112, with
 // 8192, and so more partial sums, 77 and 127).
-int32_t chunk_for(int64_t tokens, int lpg) {
-  int32_t chunk = kSumRows;
-  while (chunk < 128 && tokens * lpg > (int64_t)chunk * 2048 * kWave) chunk *= 2;
-  return chunk;
+int32_t run_for(int64_t tokens, int lpg) {
+  int32_t run = kSumRows;
+  while (run < 128 && tokens * lpg > (int64_t)run * 2048 * kWave) run *= 2;
+  return run;
 }
+int32_t chunk_for(int64_t tokens, int lpg) { return run_for(tokens, lpg) * (kThreads / lpg); }
 
 // Where a call's scratch holds what.
 size_t padded(int64_t bytes) { return (size_t)ceil_div(bytes, 256) * 256; }
@@ -775,10 +822,14 @@ int group_lanes(kbc_type type, int32_t dim) {
   return lanes_for(dim, dim >= v ? v : 1);
 }
 
-// A pooled sum takes a workgroup per bag where no bag can be long: few tokens in
-// all, or bags of one, small length.
+// A pooled sum takes a workgroup per bag where no bag can be long: bags of one, small
+// length (128 of 512 rows of 128 floats 19 us, as a segmented sum 20; 512 of 512 rows
+// of 512 bfloat16 68 and 52), or few tokens in all (one bag of 256 / 1024 / 4096 rows
+// 8 / 24 / 87 us, as a segmented sum 10 / 15 / 25; 128 bags of 11 5 and 12).
 bool pools_directly(int64_t tokens, int64_t bags, bool ragged) {
-  return bags <= kMostBlocks && (tokens <= 4096 || (!ragged && tokens / bags <= 512));
+  if (bags > kMostBlocks) return false;
+  const int64_t mean = tokens / bags;
+  return ragged ? tokens <= 512 || (tokens <= 4096 && mean <= 64) : mean <= 512;
 }
 
 void launch_sum(kbc_type type, const SumArgs &a, hipStream_t s) {
@@ -786,7 +837,7 @@ void launch_sum(kbc_type type, const SumArgs &a, hipStream_t s) {
   with_rows(type, a.dim, [&](auto t, auto vec, auto lanes) {
     using T = decltype(t);
     constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
-    const dim3 grid((unsigned)ceil_div(chunks, kThreads / L), (unsigned)ceil_div(a.dim, L * V));
+    const dim3 grid((unsigned)chunks, (unsigned)ceil_div(a.dim, L * V));
     hipLaunchKernelGGL((sum_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
   });
   if (chunks <= 1) return;
@@ -891,7 +942,7 @@ kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int
              out, bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
   const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads), 0, 1);
   hipLaunchKernelGGL(pool_list_kernel, grid, dim3(kThreads), 0, s, l);
-  const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), table, stride, dim, nullptr,
+  const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), table, stride, dim, nullptr,
                   mean ? l.weights : nullptr, scale, out, bags,
                   w + at.slots};
   launch_sum(type, a, s);
@@ -951,7 +1002,7 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
     }
   }
   if (tokens > 0) {
-    const SumArgs a{l.entries, tokens, chunk_for(tokens, lpg), dout, dim, dim,
+    const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), dout, dim, dim,
                     mean ? l.weights : nullptr, nullptr, scale, dtable, rows,
                     w + at.slots};
     launch_sum(type, a, s);

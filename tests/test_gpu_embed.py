@@ -178,6 +178,22 @@ def test_padded_bags(chain, pool, bags, length):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("tokens,dim", [(70_000, 3), (70_000, 9), (20_000, 130), (9001, 600)])
+def test_rows_that_cross_runs_and_chunks(chain, dtype, tokens, dim):
+    """Sums that end inside a lane group's run, inside a workgroup's chunk and behind
+    many chunks, in rows of every number of lanes."""
+    import torch
+    g = np.random.default_rng(tokens + dim)
+    lengths = np.concatenate([g.integers(0, 30, 400), g.integers(0, 700, 20), [tokens // 2]])
+    g.shuffle(lengths)
+    offsets = np.minimum(np.concatenate([[0], lengths.cumsum()]), tokens)
+    ids = np.sort(g.integers(-1, 900, tokens) ** 2 // 900)
+    table, dout, dev = tensors(g, 900, dim, dtype, ids, (offsets.size - 1,))
+    check(chain, table, dev, torch.from_numpy(offsets).cuda(), 1.0, "mean", dout, dtype)
+
+
+@pytest.mark.gpu
 def test_a_long_bag_is_counted(chain):
     """A mean over a bag that a whole workgroup counts, between short ones."""
     import torch
