@@ -266,6 +266,9 @@ def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
     """The gradient [rows][dim] of embed's table, of dout's type, for the upstream
     gradient dout of its output; rows that no id names are zeros."""
     code = _type(dout, "dout")
+    rows = int(rows)
+    if rows < 1:
+        raise ValueError("rows must be positive")
     device = dout.device
     bags, at = _bag_args(ids, offsets, pool, device)
     lead = tuple(ids.shape) if bags is None else (bags,)
@@ -308,7 +311,8 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     2-D ids, or with offsets (bags + 1 of them, not decreasing, of the ids' type)
     ids[offsets[g]:offsets[g + 1]] of a 1-D ids.  An id outside [0, rows) stands for
     padding: zeros, no term, not counted by the mean, no gradient; a bag of nothing
-    else is zeros.  Differentiable with respect to table.
+    else is zeros.  ids and offsets are contiguous int32 or int64; a row of table is
+    adjacent values, rows may lie apart.  Differentiable with respect to table.
     """
     if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
         return _Embed.apply(table, ids, offsets, scale, pool)

@@ -197,13 +197,21 @@ __global__ __launch_bounds__(kThreads) void pool_kernel(PoolArgs a) {
 // for a pooled sum (bag, id).  An entry whose second field is -1 adds nothing, one
 // whose first is the number of output rows is of no row.
 
+// The weights of a mean's bags: few tokens' in one launch, a wave or a workgroup a bag;
+// else in three, as a bag may hold any share of the tokens: counts cleared, tokens
+// counted (whole numbers added in any order), weights made of them.
+enum Weigh { kNone, kAtOnce, kClearCounts, kCountTokens, kWeighBags };
+
 struct ListArgs {
   Ints ids;
   Bags bags;
   int64_t tokens, rows;
   int32_t mean;
-  double *weights;  // with mean: 1 / tokens of each bag (0: none)
-  void *fill;       // output rows to clear, in words of 4 bytes and a rest of 2
+  int32_t weigh;    // with mean: which step of the bags' weights the launch takes
+  int32_t count_per;  // tokens that a thread counts
+  int32_t *counts;  // tokens of each bag
+  double *weights;  // 1 / those (0: none)
+  void *fill;       // output rows to clear
   int64_t fill_bytes;
   int2 *entries;
   // workgroups of a launch: list_wgs make the list, then weight_wgs, then those of a
@@ -263,6 +271,50 @@ __device__ void bag_weights(const ListArgs &a, int64_t block) {
   }
 }
 
+// Counts the tokens of a block of kThreads * count_per for their bags: one bag's, as in
+// a long bag, with one addition, others with one for each bag and wave.  (Additions
+// to one count take 12 ns each, one a wave 49 us for a bag of 262144.)
+__device__ void count_tokens(const ListArgs &a, int64_t block) {
+  __shared__ int counts[kWaves];
+  const int64_t first = block * kThreads * a.count_per;
+  const int64_t end = min(a.tokens, first + (int64_t)kThreads * a.count_per);
+  const int64_t g = bag_of(a.bags, first);  // the same for the whole workgroup, as what follows
+  if (g >= 0 && bag_begin(a.bags, g + 1) >= end) {
+    const int n = count_ids(a, first, end, threadIdx.x, kThreads);
+    if (threadIdx.x % kWave == 0) counts[threadIdx.x / kWave] = n;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int all = 0;
+      for (int w = 0; w < kWaves; ++w) all += counts[w];
+      if (all) atomicAdd(&a.counts[g], all);
+    }
+    return;
+  }
+  const int lane = threadIdx.x % kWave;
+  for (int64_t t0 = first + threadIdx.x - lane; t0 < end; t0 += kThreads) {  // a wave's tokens
+    const int64_t t = min(t0 + lane, end - 1), id = load_int(a.ids, t);
+    const bool valid = t0 + lane < end && id >= 0 && id < a.rows;
+    const int own = (int)bag_of(a.bags, t);  // (bags are below 2^31)
+    // A bag's tokens are neighbours: the first lane of them adds all.
+    const int before = __shfl_up(own, 1);
+    const bool begins = lane == 0 || own != before;
+    const unsigned long long behind = __ballot(begins) >> lane >> 1;
+    const int n = behind ? 1 + __builtin_ctzll(behind) : kWave - lane;
+    const unsigned long long mine = __ballot(valid) >> lane & (n < kWave ? (1ull << n) - 1 : ~0ull);
+    if (begins && own >= 0 && mine) atomicAdd(&a.counts[own], __popcll(mine));
+  }
+}
+__device__ __forceinline__ void weigh(const ListArgs &a, int64_t block) {
+  if (a.weigh == kAtOnce) return bag_weights(a, block);
+  if (a.weigh == kCountTokens) return count_tokens(a, block);
+  const int64_t g = block * kThreads + threadIdx.x;
+  if (g >= a.bags.n) return;
+  if (a.weigh == kClearCounts)
+    a.counts[g] = 0;
+  else
+    a.weights[g] = a.counts[g] > 0 ? 1.0 / (double)a.counts[g] : 0.0;
+}
+
 // 64 KB of zeros from each workgroup.
 typedef unsigned int fill_vec __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int64_t kFillBytes = 16 * kThreads * 16;
@@ -284,11 +336,13 @@ __device__ __forceinline__ bool other_work(const ListArgs &a) {
   if (blockIdx.x < a.list_wgs) return false;
   const uint32_t k = blockIdx.x - a.list_wgs;
   if (k < a.weight_wgs)
-    bag_weights(a, k);
+    weigh(a, k);
   else
     clear(a, (int64_t)a.first_fill + (k - a.weight_wgs));
   return true;
 }
+
+__global__ __launch_bounds__(kThreads) void prepare_kernel(ListArgs a) { (void)other_work(a); }
 
 // A pooled sum's list, which is in order as it is.
 __global__ __launch_bounds__(kThreads) void pool_list_kernel(ListArgs a) {
@@ -526,7 +580,7 @@ struct SumArgs {
   int64_t src_stride;
   int32_t dim;
   const double *src_weights;  // of the rows read, or null
-  const double *out_weights;  // of the rows written, or null
+  const int32_t *out_counts;  // terms of the rows written, whose mean it is, or null
   double scale;
   void *out;
   int64_t out_rows;
@@ -545,7 +599,8 @@ template <class T, int VEC>
 __device__ __forceinline__ void write_row(const SumArgs &a, int key, int c,
                                           const double (&acc)[VEC]) {
   if (key < 0 || key >= a.out_rows) return;
-  const double w = a.out_weights ? a.scale * a.out_weights[key] : a.scale;
+  // (A row of no terms is zero.)
+  const double w = a.out_counts ? a.scale / (double)max(a.out_counts[key], 1) : a.scale;
   T y[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) y[i] = round_to<T>(acc[i] * w);
@@ -795,7 +850,7 @@ int32_t chunk_for(int64_t tokens, int lpg) { return run_for(tokens, lpg) * (kThr
 // Where a call's scratch holds what.
 size_t padded(int64_t bytes) { return (size_t)ceil_div(bytes, 256) * 256; }
 struct Scratch {
-  size_t entries, sorted, counts, totals, weights, slots, bytes;
+  size_t entries, sorted, counts, totals, bag_counts, weights, slots, bytes;
 };
 Scratch scratch_for(int64_t tokens, int64_t bags, int32_t dim, bool sorted, bool mean, int lpg) {
   Scratch s = {};
@@ -811,7 +866,10 @@ Scratch scratch_for(int64_t tokens, int64_t bags, int32_t dim, bool sorted, bool
     s.counts = take(kDigits * tiles_of(tokens) * 4);
     s.totals = take(kDigits * 4);
   }
-  if (mean) s.weights = take(bags * 8);
+  if (mean) {
+    s.bag_counts = take(bags * 4);
+    s.weights = take(bags * 8);
+  }
   const int64_t chunks = ceil_div(tokens, chunk_for(tokens, lpg));
   if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);  // (half of it with 16-bit types)
   s.bytes = at;
@@ -823,9 +881,10 @@ int group_lanes(kbc_type type, int32_t dim) {
 }
 
 // A pooled sum takes a workgroup per bag where no bag can be long: bags of one, small
-// length (128 of 512 rows of 128 floats 19 us, as a segmented sum 20; 512 of 512 rows
-// of 512 bfloat16 68 and 52), or few tokens in all (one bag of 256 / 1024 / 4096 rows
-// 8 / 24 / 87 us, as a segmented sum 10 / 15 / 25; 128 bags of 11 5 and 12).
+// length (512 of 32 rows of 512 bfloat16 values 6 us, as a segmented mean 17; 2048 of
+// 128 rows of 256 22 and 41; 128 of 512 rows of 128 floats 19 and 20; 512 of 512 rows of
+// 512 bfloat16 68 and 55), or few tokens in all (one bag of 256 / 1024 / 4096 rows of
+// 128 floats 8 / 24 / 87 us, as a segmented mean 10 / 13 / 15; 128 bags of 11 5 and 12).
 bool pools_directly(int64_t tokens, int64_t bags, bool ragged) {
   if (bags > kMostBlocks) return false;
   const int64_t mean = tokens / bags;
@@ -857,13 +916,18 @@ void launch_sum(kbc_type type, const SumArgs &a, hipStream_t s) {
   }
 }
 
-// The grid of launch k of `launches` that make a list: the first also weighs the
-// bags, and each clears a share of the output.
-dim3 list_grid(ListArgs *a, int64_t list_wgs, int k, int launches) {
+// The grid of launch k of `launches` that make a list: with a mean each takes the
+// step `weigh` of the bags' weights, and each clears a share of the output.
+dim3 list_grid(ListArgs *a, int64_t list_wgs, int k, int launches, Weigh weigh) {
   const int64_t pieces = ceil_div(a->fill_bytes, kFillBytes);
   const int64_t from = pieces * k / launches, to = pieces * (k + 1) / launches;
+  a->weigh = a->mean ? weigh : kNone;
+  a->count_per = a->mean && a->tokens / a->bags.n >= kLongBag ? 8 : 1;
   a->list_wgs = (uint32_t)list_wgs;
-  a->weight_wgs = k == 0 && a->mean ? (uint32_t)ceil_div(a->bags.n, kWaves) : 0;
+  a->weight_wgs = (uint32_t)(a->weigh == kNone          ? 0
+                             : a->weigh == kAtOnce      ? ceil_div(a->bags.n, kWaves)
+                             : a->weigh == kCountTokens ? ceil_div(a->tokens, kThreads * a->count_per)
+                                                        : ceil_div(a->bags.n, kThreads));
   a->first_fill = (uint32_t)from;
   return dim3((unsigned)(list_wgs + a->weight_wgs + to - from));
 }
@@ -938,13 +1002,18 @@ kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int
   if (too_many_bags(bags, mean)) return KBC_EINVAL;
   if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
   char *w = static_cast<char *>(scratch);
-  ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, reinterpret_cast<double *>(w + at.weights),
-             out, bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
-  const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads), 0, 1);
+  ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, kNone, 1,
+             reinterpret_cast<int32_t *>(w + at.bag_counts), nullptr, out,
+             bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
+  if (mean) {  // counts cleared with the output, then counted beside the list
+    const dim3 grid = list_grid(&l, 0, 0, 1, kClearCounts);
+    hipLaunchKernelGGL(prepare_kernel, grid, dim3(kThreads), 0, s, l);
+    l.fill_bytes = 0;
+  }
+  const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads), 0, 1, kCountTokens);
   hipLaunchKernelGGL(pool_list_kernel, grid, dim3(kThreads), 0, s, l);
   const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), table, stride, dim, nullptr,
-                  mean ? l.weights : nullptr, scale, out, bags,
-                  w + at.slots};
+                  mean ? l.counts : nullptr, scale, out, bags, w + at.slots};
   launch_sum(type, a, s);
   return launched();
 }
@@ -970,11 +1039,12 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
   if (bad_scratch(at, scratch, bytes)) return KBC_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
   char *w = static_cast<char *>(scratch);
-  ListArgs l{{ids, id_bytes}, bags_of(bags, offsets, id_bytes, tokens), tokens, rows, mean,
+  ListArgs l{{ids, id_bytes}, bags_of(bags, offsets, id_bytes, tokens), tokens, rows, mean, kNone, 1,
+             reinterpret_cast<int32_t *>(w + at.bag_counts),
              reinterpret_cast<double *>(w + at.weights), dtable, rows * dim * size_of(type),
              reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
   if (tokens <= kRankTokens) {
-    const dim3 grid = list_grid(&l, ceil_div(tokens, kRankPer), 0, 1);
+    const dim3 grid = list_grid(&l, ceil_div(tokens, kRankPer), 0, 1, kAtOnce);
     hipLaunchKernelGGL(rank_kernel, grid, dim3(kThreads), (size_t)ceil_div(tokens, 4) * 16, s, l);
   } else {
     int bits = 1;
@@ -987,7 +1057,10 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
     for (int p = 0; p < passes; ++p) {
       r.bits = (bits - r.shift + (passes - p) - 1) / (passes - p);
       r.out = to[(passes - 1 - p) % 2];  // the last pass writes the entries
-      auto grid = [&](int64_t wgs, int k) { return list_grid(&r.list, wgs, p * 3 + k, passes * 3); };
+      const Weigh steps[3] = {kClearCounts, kCountTokens, kWeighBags};
+      auto grid = [&](int64_t wgs, int k) {
+        return list_grid(&r.list, wgs, p * 3 + k, passes * 3, p == 0 ? steps[k] : kNone);
+      };
       const dim3 count = grid(r.tiles, 0);
       const bool long_list = tokens >= kLongList;
       hipLaunchKernelGGL(long_list ? radix_count_kernel<8> : radix_count_kernel<2>, count,
