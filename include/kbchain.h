@@ -1,6 +1,7 @@
 /*
  * kbchain.h -- C ABI of the multi-hop chain glue (gfx950), a harness library
- * beside kbfollow.h.
+ * beside kbfollow.h, and of the operators before a hop: embedding lookup and
+ * penalties, biases and masks on logits (below).
  *
  * The multi-hop question-answering model of Sec. 3.2 chains follow steps,
  * x^t = follow(x^{t-1}, r^t), takes a softmax of the last hop's entity

@@ -398,6 +398,8 @@ kb_status kb_profile_read(kb_t *kb, double *ms, int64_t *launches);
  * launches nothing, "fill_kernel<false> + tail_kernel<...>" for a TAIL phase of
  * two launches.  residual != 0 describes kb_follow_residual and
  * kb_follow_backward_residual instead of kb_follow and kb_follow_backward.
+ * (The dR pass of a packed X has a stream kernel of its own, which this does not
+ * name.)
  * Uses the runtime's occupancy calculator on the KB's device (which must be
  * current) but enqueues nothing.  KB_EINVAL for a NULL kb or name, len = 0,
  * b < 1 or a phase outside [0, KB_PH_COUNT). */

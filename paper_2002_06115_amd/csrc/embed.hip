@@ -944,6 +944,7 @@ bool bad_scratch(const Scratch &need, const void *scratch, size_t bytes) {
   return need.bytes > 0 &&
          (!scratch || bytes < need.bytes || reinterpret_cast<uintptr_t>(scratch) % 16 != 0);
 }
+
 }  // namespace
 
 extern "C" {
@@ -1005,15 +1006,16 @@ kbc_status kbc_embed_pool(int64_t tokens, const void *ids, int32_t id_bytes, int
   ListArgs l{{ids, id_bytes}, of, tokens, rows, mean, kNone, 1,
              reinterpret_cast<int32_t *>(w + at.bag_counts), nullptr, out,
              bags * dim * size_of(type), reinterpret_cast<int2 *>(w + at.entries), 0, 0, 0};
-  if (mean) {  // counts cleared with the output, then counted beside the list
+  if (mean || tokens == 0) {  // counts cleared with the output, then counted beside the list
     const dim3 grid = list_grid(&l, 0, 0, 1, kClearCounts);
     hipLaunchKernelGGL(prepare_kernel, grid, dim3(kThreads), 0, s, l);
     l.fill_bytes = 0;
   }
+  if (tokens == 0) return launched();
   const dim3 grid = list_grid(&l, ceil_div(tokens, kThreads), 0, 1, kCountTokens);
   hipLaunchKernelGGL(pool_list_kernel, grid, dim3(kThreads), 0, s, l);
-  const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), table, stride, dim, nullptr,
-                  mean ? l.counts : nullptr, scale, out, bags, w + at.slots};
+  const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), table, stride,
+                  dim, nullptr, mean ? l.counts : nullptr, scale, out, bags, w + at.slots};
   launch_sum(type, a, s);
   return launched();
 }
@@ -1076,8 +1078,7 @@ kbc_status kbc_embed_backward(int64_t tokens, const void *ids, int32_t id_bytes,
   }
   if (tokens > 0) {
     const SumArgs a{l.entries, tokens, run_for(tokens, lpg), chunk_for(tokens, lpg), dout, dim, dim,
-                    mean ? l.weights : nullptr, nullptr, scale, dtable, rows,
-                    w + at.slots};
+                    mean ? l.weights : nullptr, nullptr, scale, dtable, rows, w + at.slots};
     launch_sum(type, a, s);
   }
   return launched();

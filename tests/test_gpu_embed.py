@@ -205,6 +205,25 @@ def test_a_long_bag_is_counted(chain):
 
 
 @pytest.mark.gpu
+def test_many_empty_bags(chain):
+    """More bags than a grid has workgroups, with no token, and with two."""
+    import torch
+    bags = 20_000_000
+    table = torch.ones((3, 2), device="cuda")
+    ids = torch.tensor([2, 1], device="cuda")
+    offsets = torch.zeros(bags + 1, dtype=torch.int64, device="cuda")
+    for pool in ("sum", "mean"):
+        assert not chain.embed(table, ids[:0], offsets, pool=pool).any()
+        offsets[-1] = 2
+        out = chain.embed(table, ids, offsets, pool=pool)
+        assert not out[:-1].any() and (out[-1] == (2.0 if pool == "sum" else 1.0)).all()
+        back = chain.embed_backward(out, ids, 3, offsets, pool=pool)
+        assert torch.equal(back[:, 0], torch.tensor([0.0, 2.0, 2.0] if pool == "sum" else
+                                                    [0.0, 0.5, 0.5], device="cuda"))
+        offsets[-1] = 0
+
+
+@pytest.mark.gpu
 def test_bad_offsets_read_nothing_outside(chain):
     """Offsets past the tokens, or negative, are taken as the nearer end."""
     import torch

@@ -195,6 +195,14 @@ def test_backward(kbf, b, weighted, path, monkeypatch):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("b", [4096, 4101])
+def test_backward_wide_rows(kbf, b):
+    """Rows past the buffer loads' stride."""
+    s, r, o, n_e, n_r = small_kb(b, n_e=40, n_t=500)
+    check_backward(kbf, s, r, o, n_e, n_r, b, None, None, b)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("b", [3, 10, 32])
 def test_backward_concurrent_passes(kbf, b, monkeypatch):
     """dR on the KB's own stream beside dX."""
