@@ -216,6 +216,12 @@ def pack(X):
         raise TypeError("X must be a float32 CUDA tensor")
     if X.dim() != 2 or X.shape[1] < 1 or not X.is_contiguous():
         raise ValueError("X must be a contiguous [rows][b] tensor")
+    return _packed(X)
+
+
+def _packed(X):
+    """pack(X) of an X that has been checked."""
+    import torch
     rows, b = X.shape
     data = torch.empty((rows, _lib.kb_packed_pitch(b)), dtype=torch.uint8, device=X.device)
     _on_device(_lib.kb_pack, "kb_pack", X.device, rows, b, X.data_ptr(), data.data_ptr())
@@ -469,10 +475,11 @@ def _make_functions():
         def forward(ctx, X, R, kb, residual):
             ctx.kb = kb
             ctx.residual = residual
+            Y = kb.follow(X, R, residual=residual)  # checks X and R
             ctx.b = X.shape[-1]
-            ctx.save_for_backward(pack(X).data if ctx.needs_input_grad[1] else None,
+            ctx.save_for_backward(_packed(X).data if ctx.needs_input_grad[1] else None,
                                   R if ctx.needs_input_grad[0] else None)
-            return kb.follow(X, R, residual=residual)
+            return Y
 
         @staticmethod
         @torch.autograd.function.once_differentiable

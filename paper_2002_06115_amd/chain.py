@@ -15,6 +15,7 @@ are embed_backward() and constrain_backward().
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -237,29 +238,52 @@ def _bag_args(ids, offsets, pool, device):
     return offsets.numel() - 1, offsets.data_ptr()
 
 
+# The scratch of a call, by its sizes.
+_pool_scratch = functools.lru_cache(maxsize=1024)(
+    lambda *sizes: _lib.kbc_embed_pool_scratch_size(*sizes))
+_gradient_scratch = functools.lru_cache(maxsize=1024)(
+    lambda *sizes: _lib.kbc_embed_backward_scratch_size(*sizes))
+
+
 def _embed_forward(table, ids, offsets, scale, pool):
+    """(out, rows, bags, type code) of embed."""
     code = _type(table, "table")
-    if table.dim() != 2 or table.shape[0] < 1 or table.shape[1] < 1:
+    if table.dim() != 2 or not table.numel():
         raise ValueError("table must be [rows][dim], not empty")
     rows, dim = table.shape
-    if (dim > 1 and table.stride(1) != 1) or (rows > 1 and table.stride(0) < dim):
+    stride, step = table.stride()
+    if (dim > 1 and step != 1) or (rows > 1 and stride < dim):
         raise ValueError("the values of a row of table must be adjacent, its rows apart")
-    stride = max(table.stride(0), dim)
     device = table.device
     bags, at = _bag_args(ids, offsets, pool, device)
     width, n = ids.element_size(), ids.numel()
     if bags is None:
         out = torch.empty((*ids.shape, dim), dtype=table.dtype, device=device)
         _run(_lib.kbc_embed, "kbc_embed", device, n, ids.data_ptr(), width, rows, dim,
-             table.data_ptr(), stride, code, float(scale), out.data_ptr())
-        return out
+             table.data_ptr(), max(stride, dim), code, float(scale), out.data_ptr())
+        return out, rows, bags, code
     out = torch.empty((bags, dim), dtype=table.dtype, device=device)
-    mean = int(pool == "mean")
-    held, scratch, size = _bytes(_lib.kbc_embed_pool_scratch_size(
-        n, bags, offsets is not None, dim, code, mean), device)
+    mean = pool == "mean"
+    held, scratch, size = _bytes(_pool_scratch(n, bags, offsets is not None, dim, code, mean),
+                                 device)
     _run(_lib.kbc_embed_pool, "kbc_embed_pool", device, n, ids.data_ptr(), width, bags, at, rows,
-         dim, table.data_ptr(), stride, code, float(scale), mean, out.data_ptr(), scratch, size)
-    return out
+         dim, table.data_ptr(), max(stride, dim), code, float(scale), mean, out.data_ptr(), scratch,
+         size)
+    return out, rows, bags, code
+
+
+def _embed_gradient(dout, ids, offsets, rows, bags, scale, mean, code):
+    """embed_backward of arguments that have been checked."""
+    device, dim, n = dout.device, dout.shape[-1], ids.numel()
+    if bags == 0:
+        n = 0  # tokens of no bag
+    bags = bags or 0
+    dtable = torch.empty((rows, dim), dtype=dout.dtype, device=device)
+    held, scratch, size = _bytes(_gradient_scratch(n, bags, dim, code, mean), device)
+    _run(_lib.kbc_embed_backward, "kbc_embed_backward", device, n, ids.data_ptr(),
+         ids.element_size(), bags, None if offsets is None else offsets.data_ptr(), rows, dim,
+         dout.data_ptr(), code, scale, mean, dtable.data_ptr(), scratch, size)
+    return dtable
 
 
 def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
@@ -269,38 +293,27 @@ def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
     rows = int(rows)
     if rows < 1:
         raise ValueError("rows must be positive")
-    device = dout.device
-    bags, at = _bag_args(ids, offsets, pool, device)
+    bags, _ = _bag_args(ids, offsets, pool, dout.device)
     lead = tuple(ids.shape) if bags is None else (bags,)
     if dout.dim() != len(lead) + 1 or tuple(dout.shape[:-1]) != lead or dout.shape[-1] < 1 or \
             not dout.is_contiguous():
         raise ValueError(f"dout must be contiguous, of shape {lead} and a row's width")
-    dim, n, mean = dout.shape[-1], ids.numel(), int(pool == "mean")
-    if bags == 0:
-        n = 0  # tokens of no bag
-    dtable = torch.empty((rows, dim), dtype=dout.dtype, device=device)
-    held, scratch, size = _bytes(_lib.kbc_embed_backward_scratch_size(
-        n, bags or 0, dim, code, mean), device)
-    _run(_lib.kbc_embed_backward, "kbc_embed_backward", device, n, ids.data_ptr(),
-         ids.element_size(), bags or 0, at, rows, dim, dout.data_ptr(), code, float(scale), mean,
-         dtable.data_ptr(), scratch, size)
-    return dtable
+    return _embed_gradient(dout, ids, offsets, rows, bags, float(scale), pool == "mean", code)
 
 
 class _Embed(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, offsets, scale, pool):
+        out, rows, bags, code = _embed_forward(table, ids, offsets, scale, pool)
         ctx.save_for_backward(ids, offsets)
-        ctx.args = table.shape[0], table.dtype, scale, pool
-        return _embed_forward(table, ids, offsets, scale, pool)
+        ctx.args = rows, bags, float(scale), pool == "mean", code
+        return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        ids, offsets = ctx.saved_tensors
-        rows, dtype, scale, pool = ctx.args
-        return (embed_backward(dout.to(dtype).contiguous(), ids, rows, offsets, scale, pool),
-                None, None, None, None)
+        dtable = _embed_gradient(dout.contiguous(), *ctx.saved_tensors, *ctx.args)
+        return dtable, None, None, None, None
 
 
 def embed(table, ids, offsets=None, scale=1.0, pool=None):
@@ -316,7 +329,7 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     """
     if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
         return _Embed.apply(table, ids, offsets, scale, pool)
-    return _embed_forward(table, ids, offsets, scale, pool)
+    return _embed_forward(table, ids, offsets, scale, pool)[0]
 
 
 # -- penalties, biases and masks on logits ----------------------------------------
@@ -372,36 +385,62 @@ def _logits(z, name):
 
 
 def _constrain_forward(z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
+    """(out, type code, the library's description) of constrain."""
     n, b, code = _logits(z, "z")
-    l = _limits(n, b, z.device, bias, allowed, history, offsets,
+    device = z.device
+    l = _limits(n, b, device, bias, allowed, history, offsets,
                 {"repeat": repeat, "presence": presence, "frequency": frequency})
-    out = torch.empty((n, b), dtype=torch.float32, device=z.device)
-    _run(_lib.kbc_constrain, "kbc_constrain", z.device, n, b, z.data_ptr(), code, l, float(fill),
+    out = torch.empty((n, b), dtype=torch.float32, device=device)
+    _run(_lib.kbc_constrain, "kbc_constrain", device, n, b, z.data_ptr(), code, l, float(fill),
          out.data_ptr())
-    return out
+    return out, code, l
+
+
+def _constrain_gradient(dout, z, l, bias_dims, dtype, code):
+    """constrain_backward of arguments that have been checked."""
+    n, b = dout.shape
+    device = dout.device
+    dz = torch.empty((n, b), dtype=dtype, device=device)
+    dbias = None if bias_dims is None else \
+        torch.empty((n,) if bias_dims == 1 else (n, b), dtype=torch.float32, device=device)
+    l.bias_each = bias_dims == 2
+    _run(_lib.kbc_constrain_backward, "kbc_constrain_backward", device, n, b,
+         None if z is None else z.data_ptr(), code, l, dout.data_ptr(), dz.data_ptr(),
+         None if dbias is None else dbias.data_ptr())
+    return dz, dbias
 
 
 class _Constrain(torch.autograd.Function):
     @staticmethod
     def forward(ctx, z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
-        out = _constrain_forward(z, bias, allowed, history, offsets, repeat, presence,
-                                 frequency, fill)
+        out, code, l = _constrain_forward(z, bias, allowed, history, offsets, repeat, presence,
+                                          frequency, fill)
         each = isinstance(repeat, torch.Tensor)
-        scaled = history is not None and (each or repeat != 1.0)
-        ctx.save_for_backward(z if scaled else None, allowed, history if scaled else None,
-                              offsets, repeat if each else None)
-        ctx.args = z.dtype, None if each else repeat, None if bias is None else bias.dim()
+        if l.entries and (each or l.repeat_all != 1.0):
+            ctx.save_for_backward(allowed, z, history, offsets, repeat if each else None)
+        else:  # the gradient knows no history
+            l.entries = 0
+            ctx.save_for_backward(allowed)
+        ctx.args = l, z.dtype, code, None if bias is None else bias.dim()
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        z, allowed, history, offsets, repeat = ctx.saved_tensors
-        dtype, repeat_all, bias_dims = ctx.args
-        dz, dbias = constrain_backward(
-            dout.contiguous(), z, allowed, history, None if history is None else offsets,
-            repeat_all if repeat is None else repeat,
-            bias_dims if ctx.needs_input_grad[1] else None, dtype)
+        allowed, *more = ctx.saved_tensors
+        l, dtype, code, bias_dims = ctx.args
+        # What was saved may have moved since; the rest the gradient does not know.
+        l = _Limits.from_buffer_copy(l)
+        l.bias = l.presence = l.frequency = z = None
+        if allowed is not None:
+            l.allowed = allowed.data_ptr()
+        if more:
+            z, history, offsets, repeat = more
+            l.history = history.data_ptr()
+            l.offsets = None if offsets is None else offsets.data_ptr()
+            l.repeat = None if repeat is None else repeat.data_ptr()
+        dz, dbias = _constrain_gradient(dout.contiguous(), z, l,
+                                        bias_dims if ctx.needs_input_grad[1] else None, dtype, code)
         return dz, dbias, None, None, None, None, None, None, None
 
 
@@ -427,7 +466,7 @@ def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0
     if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
                                        for t in (z, bias)):
         return _Constrain.apply(*args)
-    return _constrain_forward(*args)
+    return _constrain_forward(*args)[0]
 
 
 def constrain_backward(dout, z=None, allowed=None, history=None, offsets=None, repeat=1.0,
@@ -444,15 +483,10 @@ def constrain_backward(dout, z=None, allowed=None, history=None, offsets=None, r
         dtype = z.dtype
     if bias_dims not in (None, 1, 2):
         raise ValueError("bias_dims must be None, 1 or 2")
-    dz = torch.empty((n, b), dtype=dtype or torch.float32, device=device)
-    code = _type(dz, "dz")
+    dtype = dtype or torch.float32
+    if dtype not in _TYPES:
+        raise TypeError("dtype must be float32, bfloat16 or float16")
     l = _limits(n, b, device, None, allowed, history, offsets, {"repeat": repeat})
-    l.bias_each = bias_dims == 2
-    dbias = None if bias_dims is None else \
-        torch.empty((n,) if bias_dims == 1 else (n, b), dtype=torch.float32, device=device)
     if l.entries and (l.repeat or l.repeat_all != 1.0) and z is None:
         raise ValueError("z is needed where a history has a repeat")
-    _run(_lib.kbc_constrain_backward, "kbc_constrain_backward", device, n, b,
-         None if z is None else z.data_ptr(), code, l, dout.data_ptr(), dz.data_ptr(),
-         None if dbias is None else dbias.data_ptr())
-    return dz, dbias
+    return _constrain_gradient(dout, z, l, bias_dims, dtype, _TYPES[dtype])

@@ -217,6 +217,42 @@ def test_against_differences(chain):
 
 
 @pytest.mark.gpu
+def test_gradients_of_what_was_saved(chain):
+    """Two graphs at once, walked twice, after the callers' own references are gone and
+    their memory has been used again; saved tensors that hooks have moved."""
+    import torch
+    g = np.random.default_rng(17)
+
+    def graph(seed):
+        gen = np.random.default_rng(seed)
+        z = torch.from_numpy(gen.standard_normal((300, 8)).astype(np.float32)).cuda().requires_grad_()
+        history = torch.from_numpy(gen.integers(0, 300, (8, 20))).cuda()
+        allowed = torch.from_numpy(gen.random((300, 8)) < 0.7).cuda()
+        repeat = torch.from_numpy(gen.uniform(1.1, 2.0, 8).astype(np.float32)).cuda()
+        out = chain.constrain(z, allowed=allowed, history=history, repeat=repeat,
+                              presence=torch.rand(8, device="cuda"))
+        table = torch.from_numpy(gen.standard_normal((90, 5)).astype(np.float32)).cuda()
+        table.requires_grad_()
+        q = chain.embed(table, history % 90, pool="mean")
+        return (z, out), (table, q)
+
+    up = torch.from_numpy(g.standard_normal((300, 8)).astype(np.float32)).cuda()
+    uq = torch.from_numpy(g.standard_normal((8, 5)).astype(np.float32)).cuda()
+    walk = lambda s: [torch.autograd.grad(s[0][1], s[0][0], up, retain_graph=True)[0],  # noqa: E731
+                      torch.autograd.grad(s[1][1], s[1][0], uq, retain_graph=True)[0]]
+    want = [walk(graph(seed)) for seed in (1, 2)]
+    both = [graph(seed) for seed in (1, 2)]
+    junk = [torch.full((20_000,), 3, device="cuda") for _ in range(50)]
+    for _ in range(2):
+        for s, w in zip(both, want):
+            assert all(torch.equal(a, b) for a, b in zip(walk(s), w))
+    del junk
+    with torch.autograd.graph.save_on_cpu():
+        s = graph(1)
+    assert all(torch.equal(a, b) for a, b in zip(walk(s), want[0]))
+
+
+@pytest.mark.gpu
 def test_unaligned_arrays(chain):
     import torch
     g = np.random.default_rng(13)
