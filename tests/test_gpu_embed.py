@@ -414,6 +414,11 @@ def test_python_refusals_on_the_gpu(chain):
             (ValueError, lambda: chain.embed_backward(t[:3], i, 4, o, pool="sum"))]:
         with pytest.raises(error):
             call()
+    with pytest.raises(ValueError):
+        chain.embed_backward(t, i[:4], 0)
     assert chain.embed(t, i[:0]).shape == (0, 6)
+    table = t.clone().requires_grad_()
+    none = chain.embed(table, i[:0])
+    assert not torch.autograd.grad(none, table, torch.ones_like(none))[0].any()
     assert chain.embed(t, i[:0].view(0, 4), pool="mean").shape == (0, 6)
     assert not chain.embed_backward(t[:0], i, 4, o[:1], pool="sum").any()

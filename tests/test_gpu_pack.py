@@ -219,6 +219,18 @@ def test_backward_small_kbs(kbf, n_t):
 
 
 @pytest.mark.gpu
+def test_no_entities(kbf):
+    import torch
+    none = np.zeros(0, np.int32)
+    kb = kbf.KB(none, none, none, 0, 3)
+    X = torch.zeros((0, 6), device="cuda").requires_grad_()
+    R = torch.ones((3, 6), device="cuda").requires_grad_()
+    Y = kbf.follow(kb, X, R, pack=True)
+    dX, dR = torch.autograd.grad(Y, (X, R), torch.zeros_like(Y))
+    assert dX.shape == (0, 6) and dR.shape == (3, 6) and not dR.any()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("b", [3, 4, 33, 128])
 def test_checked_build_counts_nothing(kbf, b):
     import torch
