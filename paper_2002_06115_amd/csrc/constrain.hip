@@ -12,7 +12,9 @@
 // One pass over the arrays in the order they lie in, 4 elements a lane, writes every
 // element as if no history were, bound by the bytes it moves; then the few elements
 // of the history are written again, by the threads that count them.  (A dense array
-// of counts would be read and written as a whole for them.)  A column's ids are
+// of counts would be read and written as a whole for them.)  Where array and history
+// are small each workgroup counts for its own elements first, and one launch is all.
+// Otherwise a column's ids are
 // compared with each other, a block of them in LDS at a time: no table that ids
 // could overflow, nothing to clear, and an id that occurs twice is written twice
 // with the same value.  A shared bias' gradient is summed row by row, in double, in
@@ -169,7 +171,66 @@ __device__ __forceinline__ void store4(T *p, int m, const float (&y)[4]) {
   }
 }
 
-// -- every element, as if no history were ---------------------------------------------
+struct Penalties {
+  Ints ids;
+  Bags columns;
+  const float *repeat, *presence, *frequency;  // [b], or null:
+  float repeat_all, presence_all, frequency_all;
+};
+
+// The row that entry t names, -1 for padding.
+__device__ __forceinline__ int row_of(const Penalties &p, int64_t n, int64_t t) {
+  const int64_t id = load_int(p.ids, t);
+  return id >= 0 && id < n ? (int)id : -1;
+}
+
+// An element of the history, in double: the logit, and the slope of the logit.
+__device__ __forceinline__ float penalised(const Penalties &p, int32_t col, float logit, int count,
+                                           float bias) {
+  const double z = (double)logit, repeat = p.repeat ? p.repeat[col] : p.repeat_all;
+  double v = z > 0.0 ? z / repeat : z * repeat;
+  v -= p.presence ? p.presence[col] : p.presence_all;
+  v -= (double)(p.frequency ? p.frequency[col] : p.frequency_all) * count;
+  return (float)(v + (double)bias);
+}
+__device__ __forceinline__ float scaled(const Penalties &p, int32_t col, float logit, float dout) {
+  const double g = (double)dout, repeat = p.repeat ? p.repeat[col] : p.repeat_all;
+  return (float)(logit > 0.0f ? g / repeat : g * repeat);
+}
+
+// A few ids over a small array: every workgroup counts those of its own elements,
+// size of them from `first` on, in LDS.
+constexpr int kFewTile = kThreads * 4;
+constexpr int kFewColumns = 1024;
+__device__ void count_few(const Args &a, const Penalties &p, int64_t first, int size, int *counts,
+                          int *begins) {
+  for (int i = threadIdx.x; i < size; i += kThreads) counts[i] = 0;
+  if (p.columns.offsets.p)
+    for (int c = threadIdx.x; c <= a.b; c += kThreads) begins[c] = (int)bag_begin(p.columns, c);
+  __syncthreads();
+  for (int t = threadIdx.x; t < (int)p.columns.tokens; t += kThreads) {
+    const int id = row_of(p, a.n, t);
+    int col;
+    if (!p.columns.offsets.p) {
+      col = t / (int)p.columns.each;
+    } else {
+      int lo = 0, hi = a.b + 1;  // begins [0, lo) are <= t, [hi, b] are > t
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (begins[mid] <= t)
+          lo = mid + 1;
+        else
+          hi = mid;
+      }
+      col = lo - 1;
+    }
+    const int64_t f = (int64_t)id * a.b + col - first;
+    if (id >= 0 && col >= 0 && col < a.b && f >= 0 && f < size) atomicAdd(&counts[f], 1);
+  }
+  __syncthreads();
+}
+
+// -- every element, as if no history were, or with that of a few ids -----------------------
 
 // Vectors of 4 elements of a thread, and elements of a workgroup: DEPTH 1 where an
 // array is small and latency counts, 4 where it is large.
@@ -177,9 +238,11 @@ template <int DEPTH>
 constexpr int kTile = kThreads * 4 * DEPTH;
 constexpr int kMostTile = kTile<4>;
 
-// BACKWARD: dz (and a bias' own gradient, one an element) from dout.
-template <class T, bool BACKWARD, int DEPTH>
-__global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
+// BACKWARD: dz (and a bias' own gradient, one an element) from dout.  FEW: with the
+// history (DEPTH 1).
+template <class T, bool BACKWARD, int DEPTH, bool FEW>
+__global__ __launch_bounds__(kThreads) void dense_kernel(Args a, Penalties h) {
+  static_assert(!FEW || kTile<DEPTH> == kFewTile, "a count for each element");
   using In = std::conditional_t<BACKWARD, float, T>;
   using Out = std::conditional_t<BACKWARD, T, float>;
   const In *in = BACKWARD ? reinterpret_cast<const In *>(a.dout) : static_cast<const In *>(a.z);
@@ -202,32 +265,53 @@ __global__ __launch_bounds__(kThreads) void dense_kernel(Args a) {
             (int)max((int64_t)0, min((int64_t)4, size - first - local))};
     v[k] = load4<In>(in + p[k].f, p[k].m);
   }
+  __shared__ int counts[FEW ? kFewTile : 1], begins[FEW ? kFewColumns + 1 : 1];
+  if constexpr (FEW) count_few(a, h, first, kFewTile, counts, begins);
 #pragma unroll
   for (int k = 0; k < DEPTH; ++k) {
     if (p[k].m == 0) break;
     const unsigned ok = allowed4(a, p[k]);
-    float y[4];
+    float y[4], bias[4];
     if constexpr (BACKWARD) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = ok >> e & 1 ? (float)v[k][e] : 0.0f;
+      if (a.dbias) store4<float>(a.dbias + p[k].f, p[k].m, y);
     } else {
-      bias4(a, p[k], y);
+      bias4(a, p[k], bias);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = ok >> e & 1 ? (float)v[k][e] + y[e] : a.fill;
+      for (int e = 0; e < 4; ++e) y[e] = ok >> e & 1 ? (float)v[k][e] + bias[e] : a.fill;
+    }
+    if constexpr (FEW) {
+      int32_t col = p[k].col;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (e < p[k].m && (ok >> e & 1)) {
+          const int count = counts[threadIdx.x * 4 + e];
+          if (count > 0) {
+            if constexpr (BACKWARD)
+              y[e] = scaled(h, col, (float)static_cast<const T *>(a.z)[p[k].f + e], y[e]);
+            else
+              y[e] = penalised(h, col, (float)v[k][e], count, bias[e]);
+          }
+        }
+        if (++col == a.b) col = 0;
+      }
     }
     store4<Out>(out + p[k].f, p[k].m, y);
-    if constexpr (BACKWARD)
-      if (a.dbias) store4<float>(a.dbias + p[k].f, p[k].m, y);
   }
 }
 
 // The backward pass with a shared bias: G lanes a row, which they also sum.  (Four
 // rows of a group in flight took as long for 64 million elements, and 16.8 us for
 // 14.8 for 4 million, with the history's launch.)
-template <class T, int G>
-__global__ __launch_bounds__(kThreads) void row_kernel(Args a) {
+template <class T, int G, bool FEW>
+__global__ __launch_bounds__(kThreads) void row_kernel(Args a, Penalties h) {
+  constexpr int GPB = kThreads / G;
+  __shared__ int counts[FEW ? kFewTile : 1], begins[FEW ? kFewColumns + 1 : 1];
+  if constexpr (FEW)  // (b is at most 4 G)
+    count_few(a, h, (int64_t)blockIdx.x * GPB * a.b, GPB * a.b, counts, begins);
   const int lane = threadIdx.x % G;
-  const int64_t i = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
+  const int64_t i = (int64_t)blockIdx.x * GPB + threadIdx.x / G;
   if (i >= a.n) return;  // whole groups; their shuffles stay inside the group
   double sum = 0.0;
   for (int64_t c = lane * 4; c < a.b; c += G * 4) {
@@ -239,6 +323,9 @@ __global__ __launch_bounds__(kThreads) void row_kernel(Args a) {
     for (int e = 0; e < 4; ++e) {
       y[e] = ok >> e & 1 ? v[e] : 0.0f;  // (those past the row are zeros)
       sum += (double)y[e];
+      if constexpr (FEW)
+        if (e < p.m && (ok >> e & 1) && counts[(int)(threadIdx.x / G) * a.b + (int)c + e] > 0)
+          y[e] = scaled(h, (int32_t)c + e, (float)static_cast<const T *>(a.z)[p.f + e], y[e]);
     }
     store4<T>(static_cast<T *>(a.out) + p.f, p.m, y);
   }
@@ -249,12 +336,6 @@ __global__ __launch_bounds__(kThreads) void row_kernel(Args a) {
 
 // -- the elements of the history --------------------------------------------------------
 
-struct Penalties {
-  Ints ids;
-  Bags columns;
-  const float *repeat, *presence, *frequency;  // [b], or null:
-  float repeat_all, presence_all, frequency_all;
-};
 
 // Lanes that share an entry's count: 15200 ids of 8 columns take 14 us with 16 lanes,
 // 17 with 8, 27 with 4.
@@ -262,12 +343,6 @@ constexpr int kEntryLanes = 16;
 constexpr int kEntries = kThreads / kEntryLanes;     // entries of a workgroup
 constexpr int kBlockIds = 2048;                      // ids in LDS at a time
 constexpr int kCompare = 4;                          // quads of them in flight
-
-// The row that entry t names, -1 for padding.
-__device__ __forceinline__ int row_of(const Penalties &p, int64_t n, int64_t t) {
-  const int64_t id = load_int(p.ids, t);
-  return id >= 0 && id < n ? (int)id : -1;
-}
 
 template <class T, bool BACKWARD>
 __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) {
@@ -337,18 +412,12 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
   if (!valid || lane != 0) return;
   const int64_t f = (int64_t)id * a.b + col;
   const bool ok = is_allowed(a, id, (int32_t)col);
-  const double repeat = p.repeat ? p.repeat[col] : p.repeat_all;
-  const double z = (double)(float)static_cast<const T *>(a.z)[f];
-  if constexpr (BACKWARD) {
-    const double g = a.dout[f];
-    static_cast<T *>(a.out)[f] = (T)(ok ? (float)(z > 0.0 ? g / repeat : g * repeat) : 0.0f);
-  } else {
-    double v = z > 0.0 ? z / repeat : z * repeat;
-    v -= p.presence ? p.presence[col] : p.presence_all;
-    if (counts) v -= (double)(p.frequency ? p.frequency[col] : p.frequency_all) * count;
-    v += (double)bias_of(a, id, (int32_t)col);
-    static_cast<float *>(a.out)[f] = ok ? (float)v : a.fill;
-  }
+  const float z = (float)static_cast<const T *>(a.z)[f];
+  if constexpr (BACKWARD)
+    static_cast<T *>(a.out)[f] = (T)(ok ? scaled(p, (int32_t)col, z, a.dout[f]) : 0.0f);
+  else
+    static_cast<float *>(a.out)[f] =
+        ok ? penalised(p, (int32_t)col, z, count, bias_of(a, id, (int32_t)col)) : a.fill;
 }
 
 // -- how a call is launched ----------------------------------------------------------------
@@ -398,14 +467,35 @@ Penalties penalties_for(int32_t b, const kbc_limits *l) {
 }
 
 template <class T, bool BACKWARD>
-void launch_dense(const Args &a, hipStream_t s) {
+void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
+  hipLaunchKernelGGL((history_kernel<T, BACKWARD>),
+                     dim3((unsigned)ceil_div(h.columns.tokens, kEntries)), dim3(kThreads), 0, s, a,
+                     h);
+}
+
+// Few ids over a small array, which every workgroup then reads: at most 1024, and 2^28
+// for ids times elements.  One launch against two, forward us: 256 ids over 18 x 128
+// 5.8 and 8.0, 700 over 32000 x 1 6.2 and 8.7, 279 over 8000 x 93 6.4 and 8.7; 1000 over
+// 1000 x 1000 9.4 and 9.1, 279 over 43000 x 93 11.7 and 10.5 (not taken).
+bool few_ids(const Args &a, const kbc_limits *l) {
+  return l->entries <= 1024 && a.b <= kFewColumns &&
+         a.n * a.b <= (int64_t(1) << 28) / l->entries;
+}
+
+// history: with the ids' penalties (forward), or slopes (backward).
+template <class T, bool BACKWARD>
+void launch_dense(const Args &a, bool history, const kbc_limits *l, hipStream_t s) {
   const int64_t size = a.n * a.b;
+  const Penalties h = penalties_for(a.b, l);
+  auto go = [&](auto kernel, int tile) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(size, tile)), dim3(kThreads), 0, s, a, h);
+  };
+  if (history && few_ids(a, l)) return go(dense_kernel<T, BACKWARD, 1, true>, kTile<1>);
   if (size < kSmall)
-    hipLaunchKernelGGL((dense_kernel<T, BACKWARD, 1>), dim3((unsigned)ceil_div(size, kTile<1>)),
-                       dim3(kThreads), 0, s, a);
+    go(dense_kernel<T, BACKWARD, 1, false>, kTile<1>);
   else
-    hipLaunchKernelGGL((dense_kernel<T, BACKWARD, 4>), dim3((unsigned)ceil_div(size, kTile<4>)),
-                       dim3(kThreads), 0, s, a);
+    go(dense_kernel<T, BACKWARD, 4, false>, kTile<4>);
+  if (history) launch_history<T, BACKWARD>(a, h, s);
 }
 
 // Lanes of a row in row_kernel: 4 elements each, or 4 at a time.
@@ -415,19 +505,26 @@ int row_lanes(int32_t b) {
   return lanes;
 }
 
-template <class T>
-void launch_rows(const Args &a, hipStream_t s) {
+template <class T, bool FEW>
+void launch_rows(const Args &a, const Penalties &h, hipStream_t s) {
   const int lanes = row_lanes(a.b);
   const dim3 grid((unsigned)ceil_div(a.n, kThreads / lanes));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a); };
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a, h); };
   switch (lanes) {
-    case 2: go(row_kernel<T, 2>); break;
-    case 4: go(row_kernel<T, 4>); break;
-    case 8: go(row_kernel<T, 8>); break;
-    case 16: go(row_kernel<T, 16>); break;
-    case 32: go(row_kernel<T, 32>); break;
-    default: go(row_kernel<T, 64>); break;
+    case 2: go(row_kernel<T, 2, FEW>); break;
+    case 4: go(row_kernel<T, 4, FEW>); break;
+    case 8: go(row_kernel<T, 8, FEW>); break;
+    case 16: go(row_kernel<T, 16, FEW>); break;
+    case 32: go(row_kernel<T, 32, FEW>); break;
+    default: go(row_kernel<T, 64, FEW>); break;
   }
+}
+template <class T>
+void launch_rows(const Args &a, bool history, const kbc_limits *l, hipStream_t s) {
+  const Penalties h = penalties_for(a.b, l);
+  if (history && few_ids(a, l) && a.b <= 4 * kWave) return launch_rows<T, true>(a, h, s);
+  launch_rows<T, false>(a, h, s);
+  if (history) launch_history<T, true>(a, h, s);
 }
 
 }  // namespace
@@ -447,10 +544,7 @@ kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, con
                                             l->frequency_all != 0.0f);
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    launch_dense<T, false>(a, s);
-    if (penalised)
-      hipLaunchKernelGGL((history_kernel<T, false>), dim3((unsigned)ceil_div(l->entries, kEntries)),
-                         dim3(kThreads), 0, s, a, penalties_for(b, l));
+    launch_dense<T, false>(a, penalised, l, s);
   });
   return launched();
 }
@@ -471,14 +565,10 @@ kbc_status kbc_constrain_backward(int64_t n, int32_t b, const void *z, kbc_type 
   a.dbias = dbias;
   with_type(type, [&](auto t) {
     using T = decltype(t);
-    if (shared) {
-      launch_rows<T>(a, s);
-    } else {
-      launch_dense<T, true>(a, s);
-    }
-    if (scaled)
-      hipLaunchKernelGGL((history_kernel<T, true>), dim3((unsigned)ceil_div(l->entries, kEntries)),
-                         dim3(kThreads), 0, s, a, penalties_for(b, l));
+    if (shared)
+      launch_rows<T>(a, scaled, l, s);
+    else
+      launch_dense<T, true>(a, scaled, l, s);
   });
   return launched();
 }

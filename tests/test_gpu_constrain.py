@@ -155,6 +155,17 @@ def test_types_and_biases(chain, dtype, bias):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("mask", ["none", "bool", "bits_row"])
+@pytest.mark.parametrize("bias", ["none", "row", "each"])
+@pytest.mark.parametrize("n,b,length", [(1, 1, 1024), (3, 1, 1025), (2000, 1024, 1), (70, 1025, 1),
+                                        (600, 256, 4), (600, 257, 3), (1023, 2, 512), (9, 340, 3)])
+def test_few_and_many_ids(chain, n, b, length, bias, mask):
+    """At and past the sizes where one launch does both."""
+    g = np.random.default_rng(n + b + length)
+    run(chain, g, n, b, ["float32", "bfloat16"][n % 2], bias, mask, n % 2 == 0, length)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("ragged", [False, True])
 @pytest.mark.parametrize("length,b", [(1, 5), (31, 3), (33, 2), (2047, 1), (2049, 2), (5000, 3)])
 def test_long_histories(chain, length, b, ragged):
