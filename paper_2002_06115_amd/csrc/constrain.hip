@@ -14,13 +14,13 @@
 // of the history are written again, by the threads that count them.  (A dense array
 // of counts would be read and written as a whole for them.)  Where array and history
 // are small each workgroup counts for its own elements first, and one launch is all.
-// Otherwise a column's ids are
-// compared with each other, a block of them in LDS at a time: no table that ids
-// could overflow, nothing to clear, and an id that occurs twice is written twice
-// with the same value.  A shared bias' gradient is summed row by row, in double, in
-// a fixed order, by the lanes that write the row.
+// Otherwise a short column's ids are compared with each other, a block of them in LDS
+// at a time, where an id that occurs twice is written twice with the same value, and
+// a long column's are counted in a table in LDS.  A shared bias' gradient is summed row
+// by row, in double, in a fixed order, by the lanes that write the row.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <type_traits>
@@ -336,7 +336,6 @@ __global__ __launch_bounds__(kThreads) void row_kernel(Args a, Penalties h) {
 
 // -- the elements of the history --------------------------------------------------------
 
-
 // Lanes that share an entry's count: 15200 ids of 8 columns take 14 us with 16 lanes,
 // 17 with 8, 27 with 4.
 constexpr int kEntryLanes = 16;
@@ -420,6 +419,85 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
         ok ? penalised(p, (int32_t)col, z, count, bias_of(a, id, (int32_t)col)) : a.fill;
 }
 
+// The forward pass where columns have many ids: a workgroup puts a column's ids
+// into a table in LDS and counts them there, a slice of the ids at a time (by hash,
+// at most about half as many as the table holds), then each place of the table writes
+// its element.  An id that finds no place is counted by reading the column again; a
+// place once taken stays so, so either all or none of an id's entries find theirs.
+// (1024 threads and 4096 places: 128 columns of 4000 ids 35 us for 29, 1024 of 64 30 for
+// 24, one of 16000 19 for 19.)
+constexpr int kTableThreads = 512;
+constexpr int kTable = kTableThreads * 4;
+constexpr int kSlice = kTable / 2;
+constexpr int kProbes = 256;
+
+template <class T>
+__global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties p, int parts) {
+  __shared__ int4 keys4[kTableThreads], counts4[kTableThreads];
+  int *keys = reinterpret_cast<int *>(keys4), *counts = reinterpret_cast<int *>(counts4);
+  const int32_t col = (int32_t)blockIdx.x / parts;
+  const int64_t begin = bag_begin(p.columns, col), end = bag_begin(p.columns, col + 1);
+  const int slices = end > begin ? max(parts, (int)((end - begin + kSlice - 1) / kSlice)) : 0;
+  // What an element is made of, and its place once its ids are counted.
+  struct Element {
+    float z, bias;
+    bool ok;
+  };
+  auto element = [&](int id) {
+    return Element{(float)static_cast<const T *>(a.z)[(int64_t)id * a.b + col], bias_of(a, id, col),
+                   is_allowed(a, id, col)};
+  };
+  auto write = [&](int id, int count, const Element &e) {
+    static_cast<float *>(a.out)[(int64_t)id * a.b + col] =
+        e.ok ? penalised(p, col, e.z, count, e.bias) : a.fill;
+  };
+  for (int slice = (int)blockIdx.x % parts; slice < slices; slice += parts) {
+    // (A thread clears the places that it read in the slice before.)
+    keys4[threadIdx.x] = {-1, -1, -1, -1};
+    counts4[threadIdx.x] = {0, 0, 0, 0};
+    __syncthreads();
+    for (int64_t r = begin; r < end; r += kTable) {
+      int id[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t t = r + u * kTableThreads + threadIdx.x;
+        id[u] = row_of(p, a.n, min(t, end - 1));
+        if (t >= end) id[u] = -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (id[u] < 0) continue;
+        // Two multiplications by odd numbers (2^32 over the golden ratio) spread the ids.
+        uint32_t hash = (uint32_t)id[u] * 0x9E3779B9u;
+        hash = (hash ^ hash >> 15) * 0x9E3779B9u;
+        if ((int)__umulhi(hash << 12 | hash >> 20, (uint32_t)slices) != slice) continue;
+        int at = (int)(hash % kTable), probe = 0;
+        for (; probe < kProbes; ++probe, at = (at + 1) % kTable) {
+          int key = keys[at];
+          if (key == -1) key = atomicCAS(&keys[at], -1, id[u]);
+          if (key == -1 || key == id[u]) break;
+        }
+        if (probe < kProbes) {
+          atomicAdd(&counts[at], 1);
+        } else {
+          int count = 0;
+          for (int64_t t = begin; t < end; ++t) count += row_of(p, a.n, t) == id[u];
+          write(id[u], count, element(id[u]));
+        }
+      }
+    }
+    __syncthreads();
+    const int4 k = keys4[threadIdx.x], c = counts4[threadIdx.x];
+    const int id[4] = {k.x, k.y, k.z, k.w}, count[4] = {c.x, c.y, c.z, c.w};
+    Element e[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) e[u] = element(max(id[u], 0));  // all four on their way
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (id[u] >= 0) write(id[u], count[u], e[u]);
+  }
+}
+
 // -- how a call is launched ----------------------------------------------------------------
 
 // Elements from which workgroups take 4 vectors a thread: 64 million take 81 us with
@@ -466,10 +544,31 @@ Penalties penalties_for(int32_t b, const kbc_limits *l) {
           l->repeat, l->presence, l->frequency, l->repeat_all, l->presence_all, l->frequency_all};
 }
 
+// Ids of a column, on average, from which table_kernel counts them.  With the dense
+// launch, compared and by table, us: 32 columns of 128 ids 9.6 and 9.6, of 512 11.3 and
+// 10.7, 8 of 1900 13.4 and 9.7, 1 of 16000 34 and 19, of 100000 755 and 52, 128 of 1000 37
+// and 17, of 4000 196 and 29, 1024 of 64 29 and 24; but 93 of 32 9.7 and 9.8, 20000 of 64
+// 240 and 117, of 16 70 and 109.
+constexpr int64_t kLongColumn = 64;
+// Few columns are shared by workgroups that take a slice each, up to this many in all,
+// of 512 ids at least (8 columns of 1900 in slices of 1024 9.9 us, 512 9.7, 256 10.3; one of
+// 16000 22, 19 and 17, one of 100000 60, 52 and 55).
+constexpr int64_t kTableBlocks = 512;
+constexpr int64_t kShare = 512;
+
 template <class T, bool BACKWARD>
 void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
+  const int64_t total = h.columns.tokens;
+  if constexpr (!BACKWARD)
+    if ((h.frequency || h.frequency_all != 0.0f) && total / a.b >= kLongColumn &&
+        a.b <= kMostBlocks / 4) {
+      const int64_t parts = std::clamp<int64_t>(kTableBlocks / a.b, 1, ceil_div(total, kShare));
+      hipLaunchKernelGGL((table_kernel<T>), dim3((unsigned)(a.b * parts)), dim3(kTableThreads), 0,
+                         s, a, h, (int)parts);
+      return;
+    }
   hipLaunchKernelGGL((history_kernel<T, BACKWARD>),
-                     dim3((unsigned)ceil_div(h.columns.tokens, kEntries)), dim3(kThreads), 0, s, a,
+                     dim3((unsigned)ceil_div(total, kEntries)), dim3(kThreads), 0, s, a,
                      h);
 }
 

@@ -175,6 +175,47 @@ def test_long_histories(chain, length, b, ragged):
     run(chain, g, 900, b, "float32", "row", "bool", ragged, length)
 
 
+def spread(ids):
+    """The 32 bits that a column's table takes the place (the lower 11) and the slice
+    (from bit 19 down) of an id from."""
+    h = ids.astype(np.uint32) * np.uint32(0x9E3779B9)
+    return (h ^ h >> np.uint32(15)) * np.uint32(0x9E3779B9)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["any", "one place", "one slice", "one id"])
+@pytest.mark.parametrize("n,b,length", [(300_000, 1, 1800), (300_000, 3, 2049), (400_000, 2, 9000),
+                                        (20_000, 600, 64), (50_000, 9, 130)])
+def test_histories_of_many_ids(chain, n, b, length, kind):
+    """Columns of up to thousands of different ids, also where their places in a
+    table collide, more than it has; a column of one id, an empty one, and padding."""
+    import torch
+    g = np.random.default_rng(n + b + length)
+    ids = np.arange(n)
+    if kind == "one place":
+        ids = ids[spread(ids) % 2048 < 8]
+    elif kind == "one slice":
+        ids = ids[spread(ids) >> 14 & 63 == 63]
+    elif kind == "one id":
+        ids = ids[-1:]
+    history = g.choice(ids, b * length)
+    history[::7] = history[0]
+    history[5::11] = -1
+    offsets = np.arange(b + 1) * length
+    if b > 2:
+        offsets[1] = offsets[2]
+    z = torch.from_numpy(g.standard_normal((n, b)).astype(np.float32)).cuda()
+    allowed = g.random(n) < 0.9
+    c = counts(history, offsets, n, b)
+    pen = [g.uniform(lo, hi, b).astype(np.float32) for lo, hi in ((0.7, 1.6), (0, 1), (-0.1, 0.4))]
+    want, _, _ = oracle(z.double().cpu().numpy(), None, allowed, c,
+                        *[p.astype(np.float64) for p in pen], -1e9, np.zeros((n, b)))
+    got = chain.constrain(z, history=cuda(history), offsets=cuda(offsets), allowed=cuda(allowed),
+                          repeat=cuda(pen[0]), presence=cuda(pen[1]), frequency=cuda(pen[2]),
+                          fill=-1e9)
+    close(got, want, 2.0 ** -24, "out", 2.0 ** -149)
+
+
 @pytest.mark.gpu
 def test_numbers_for_all_columns(chain):
     g = np.random.default_rng(11)
