@@ -337,21 +337,24 @@ __global__ __launch_bounds__(kThreads) void row_kernel(Args a, Penalties h) {
 // -- the elements of the history --------------------------------------------------------
 
 // Lanes that share an entry's count: 15200 ids of 8 columns take 14 us with 16 lanes,
-// 17 with 8, 27 with 4.
-constexpr int kEntryLanes = 16;
-constexpr int kEntries = kThreads / kEntryLanes;     // entries of a workgroup
+// 17 with 8, 27 with 4.  Where nothing is counted they only find the entry's column: 16
+// / 8 / 4 / 1 lanes take, with the dense launch, 8.3 / 8.6 / 8.5 / 9.5 us for 93 columns of
+// 3 ids, 55.6 / 38.3 / 28.7 / 25.7 for 128 of 4000, 49 / 35 / 30 / 22 for 20000 of 16.
+constexpr int kCountLanes = 16;
+constexpr int kFindLanes = 4;
 constexpr int kBlockIds = 2048;                      // ids in LDS at a time
 constexpr int kCompare = 4;                          // quads of them in flight
 
-template <class T, bool BACKWARD>
+template <class T, bool BACKWARD, int LANES>
 __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) {
+  constexpr int kEntries = kThreads / LANES;  // of a workgroup
   __shared__ int4 lds[kBlockIds / 4];
   __shared__ int64_t range[2];
   int *ids = reinterpret_cast<int *>(lds);
-  const int lane = threadIdx.x % kEntryLanes;
-  const int64_t t0 = (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / kEntryLanes;
+  const int lane = threadIdx.x % LANES;
+  const int64_t t0 = (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / LANES;
   const int64_t total = p.columns.tokens;
-  const int64_t col = t < total ? bag_of_lanes<kEntryLanes>(p.columns, t, lane) : -1;
+  const int64_t col = t < total ? bag_of_lanes<LANES>(p.columns, t, lane) : -1;
   int id = -1;
   int64_t begin = t, end = t + 1;  // the ids of the entry's column
   if (col >= 0) {
@@ -388,15 +391,15 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
         // Whole quads of the column, kCompare in flight, then its ends one by one.
         const int q0 = (lo + 3) / 4, q1 = hi / 4;
         int q = q0 + lane;
-        for (; q + (kCompare - 1) * kEntryLanes < q1; q += kCompare * kEntryLanes) {
+        for (; q + (kCompare - 1) * LANES < q1; q += kCompare * LANES) {
           int4 x[kCompare];
 #pragma unroll
-          for (int u = 0; u < kCompare; ++u) x[u] = lds[q + u * kEntryLanes];
+          for (int u = 0; u < kCompare; ++u) x[u] = lds[q + u * LANES];
 #pragma unroll
           for (int u = 0; u < kCompare; ++u)
             count += (x[u].x == id) + (x[u].y == id) + (x[u].z == id) + (x[u].w == id);
         }
-        for (; q < q1; q += kEntryLanes) {
+        for (; q < q1; q += LANES) {
           const int4 x = lds[q];
           count += (x.x == id) + (x.y == id) + (x.z == id) + (x.w == id);
         }
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
       }
     }
 #pragma unroll
-    for (int m = 1; m < kEntryLanes; m <<= 1) count += __shfl_xor(count, m);
+    for (int m = 1; m < LANES; m <<= 1) count += __shfl_xor(count, m);
   }
   if (!valid || lane != 0) return;
   const int64_t f = (int64_t)id * a.b + col;
@@ -559,17 +562,22 @@ constexpr int64_t kShare = 512;
 template <class T, bool BACKWARD>
 void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
   const int64_t total = h.columns.tokens;
+  const bool counts = !BACKWARD && (h.frequency || h.frequency_all != 0.0f);
   if constexpr (!BACKWARD)
-    if ((h.frequency || h.frequency_all != 0.0f) && total / a.b >= kLongColumn &&
-        a.b <= kMostBlocks / 4) {
+    if (counts && total / a.b >= kLongColumn && a.b <= kMostBlocks / 4) {
       const int64_t parts = std::clamp<int64_t>(kTableBlocks / a.b, 1, ceil_div(total, kShare));
       hipLaunchKernelGGL((table_kernel<T>), dim3((unsigned)(a.b * parts)), dim3(kTableThreads), 0,
                          s, a, h, (int)parts);
       return;
     }
-  hipLaunchKernelGGL((history_kernel<T, BACKWARD>),
-                     dim3((unsigned)ceil_div(total, kEntries)), dim3(kThreads), 0, s, a,
-                     h);
+  auto go = [&](auto kernel, int lanes) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(total, kThreads / lanes)), dim3(kThreads), 0,
+                       s, a, h);
+  };
+  if (counts)
+    go(history_kernel<T, BACKWARD, kCountLanes>, kCountLanes);
+  else
+    go(history_kernel<T, BACKWARD, kFindLanes>, kFindLanes);
 }
 
 // Few ids over a small array, which every workgroup then reads: at most 1024, and 2^28

@@ -217,6 +217,31 @@ def test_histories_of_many_ids(chain, n, b, length, kind):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("penalty", ["repeat", "presence"])
+@pytest.mark.parametrize("n,b,length", [(9000, 7, 900), (400, 130, 21), (60, 900, 3), (4000, 1, 5000)])
+def test_histories_that_nothing_counts(chain, n, b, length, penalty):
+    """Only whether an id occurs matters: ragged columns, empty ones, one of half the ids."""
+    import torch
+    g = np.random.default_rng(n + b)
+    history = g.integers(-2, n + 2, b * length)
+    offsets = np.sort(g.integers(0, b * length + 1, b + 1))
+    offsets[0], offsets[-1] = 0, b * length
+    offsets[1:b // 2] = min(offsets[1:b // 2], default=0)
+    z = torch.from_numpy(g.standard_normal((n, b)).astype(np.float32)).cuda()
+    args = dict(repeat=np.ones(b), presence=np.zeros(b))
+    args[penalty] = g.uniform(0.5, 2, b).astype(np.float32).astype(np.float64)
+    dout = g.standard_normal((n, b)).astype(np.float32)
+    want, dz, _ = oracle(z.double().cpu().numpy(), None, None, counts(history, offsets, n, b),
+                         args["repeat"], args["presence"], 0.0, 0.0, dout.astype(np.float64))
+    zg = z.requires_grad_()
+    got = chain.constrain(zg, history=cuda(history), offsets=cuda(offsets),
+                          **{penalty: cuda(args[penalty].astype(np.float32))})
+    close(got.detach(), want, 2.0 ** -24, "out", 2.0 ** -149)
+    got, = torch.autograd.grad(got, zg, cuda(dout))
+    close(got, dz, ROUND["float32"] + 2.0 ** -23, "dz", 2.0 ** -149)
+
+
+@pytest.mark.gpu
 def test_numbers_for_all_columns(chain):
     g = np.random.default_rng(11)
     run(chain, g, 200, 9, "float32", "each", "bool_row", True, 12, scalars=True)
