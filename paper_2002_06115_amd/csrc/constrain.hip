@@ -25,6 +25,7 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "id_table.h"
 #include "ids.h"
 #include "kbchain.h"
 
@@ -425,18 +426,15 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
 // The forward pass where columns have many ids: a workgroup puts a column's ids
 // into a table in LDS and counts them there, a slice of the ids at a time (by hash,
 // at most about half as many as the table holds), then each place of the table writes
-// its element.  An id that finds no place is counted by reading the column again; a
-// place once taken stays so, so either all or none of an id's entries find theirs.
+// its element.  Where an id finds no place, as ids chosen for it can bring about, the
+// slice is taken again by ranges of the id, an eighth as wide each time, until the
+// table holds them; at the latest a range has a place for each of its ids.
 // (1024 threads and 4096 places: 128 columns of 4000 ids 35 us for 29, 1024 of 64 30 for
 // 24, one of 16000 19 for 19.)
-constexpr int kTableThreads = 512;
-constexpr int kTable = kTableThreads * 4;
-constexpr int kSlice = kTable / 2;
-constexpr int kProbes = 256;
-
 template <class T>
 __global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties p, int parts) {
   __shared__ int4 keys4[kTableThreads], counts4[kTableThreads];
+  __shared__ int full;  // the last turn in which an id found no place
   int *keys = reinterpret_cast<int *>(keys4), *counts = reinterpret_cast<int *>(counts4);
   const int32_t col = (int32_t)blockIdx.x / parts;
   const int64_t begin = bag_begin(p.columns, col), end = bag_begin(p.columns, col + 1);
@@ -454,8 +452,13 @@ __global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties 
     static_cast<float *>(a.out)[(int64_t)id * a.b + col] =
         e.ok ? penalised(p, col, e.z, count, e.bias) : a.fill;
   };
-  for (int slice = (int)blockIdx.x % parts; slice < slices; slice += parts) {
-    // (A thread clears the places that it read in the slice before.)
+  if (threadIdx.x == 0) full = 0;
+  int turn = 0;
+  // The ids of [lo, lo + width) in the slice; false where the table cannot hold them.
+  auto count_range = [&](int slice, int lo, uint32_t width) {
+    const bool own_places = width <= (uint32_t)kTable;
+    ++turn;
+    // (A thread clears the places that it read the last time.)
     keys4[threadIdx.x] = {-1, -1, -1, -1};
     counts4[threadIdx.x] = {0, 0, 0, 0};
     __syncthreads();
@@ -469,27 +472,23 @@ __global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties 
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (id[u] < 0) continue;
-        // Two multiplications by odd numbers (2^32 over the golden ratio) spread the ids.
-        uint32_t hash = (uint32_t)id[u] * 0x9E3779B9u;
-        hash = (hash ^ hash >> 15) * 0x9E3779B9u;
-        if ((int)__umulhi(hash << 12 | hash >> 20, (uint32_t)slices) != slice) continue;
-        int at = (int)(hash % kTable), probe = 0;
+        if ((uint32_t)id[u] - (uint32_t)lo >= width) continue;  // padding, too
+        const uint32_t hash = id_hash((uint32_t)id[u]);
+        if (id_slice(hash, (uint32_t)slices) != slice) continue;
+        int at = own_places ? id[u] - lo : id_place(hash), probe = 0;
         for (; probe < kProbes; ++probe, at = (at + 1) % kTable) {
           int key = keys[at];
           if (key == -1) key = atomicCAS(&keys[at], -1, id[u]);
           if (key == -1 || key == id[u]) break;
         }
-        if (probe < kProbes) {
+        if (probe < kProbes)
           atomicAdd(&counts[at], 1);
-        } else {
-          int count = 0;
-          for (int64_t t = begin; t < end; ++t) count += row_of(p, a.n, t) == id[u];
-          write(id[u], count, element(id[u]));
-        }
+        else
+          full = turn;
       }
     }
     __syncthreads();
+    if (full == turn) return false;  // the same for the whole workgroup
     const int4 k = keys4[threadIdx.x], c = counts4[threadIdx.x];
     const int id[4] = {k.x, k.y, k.z, k.w}, count[4] = {c.x, c.y, c.z, c.w};
     Element e[4];
@@ -498,6 +497,19 @@ __global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties 
 #pragma unroll
     for (int u = 0; u < 4; ++u)
       if (id[u] >= 0) write(id[u], count[u], e[u]);
+    return true;
+  };
+  for (int slice = (int)blockIdx.x % parts; slice < slices; slice += parts) {
+    // 2^bits ranges (at most 8 n / kTable, so the products fit).
+    for (int64_t r = 0, bits = 0; r >> bits == 0;) {
+      const int64_t lo = a.n * r >> bits, hi = a.n * (r + 1) >> bits;
+      if (count_range(slice, (int)lo, (uint32_t)(hi - lo))) {
+        ++r;
+      } else {  // what is left, in narrower ranges
+        bits += 3;
+        r <<= 3;
+      }
+    }
   }
 }
 

@@ -1,0 +1,95 @@
+"""Long and uneven histories of chain.constrain, against the formulas in 64 bits (torch,
+on the GPU).
+
+Tolerances: an element of a history is computed in double and rounded to float once, every
+other is the logit itself: half a step, 2^-24 of the value, or 2^-150.
+"""
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def chain():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2002_06115_amd import chain
+    return chain
+
+
+PENALTIES = dict(repeat=1.3, presence=0.5, frequency=0.25)
+
+
+def check(chain, n, b, history, offsets, seed, **penalties):
+    """constrain of random logits [n][b] with this history (numpy, ids in [0, n) and
+    -1) against the formula, all elements."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    z = 3 * torch.randn((n, b), device="cuda", generator=gen)
+    h = torch.from_numpy(np.ascontiguousarray(history)).cuda()
+    o = None if offsets is None else torch.from_numpy(np.ascontiguousarray(offsets)).cuda()
+    got = chain.constrain(z, history=h, offsets=o, **penalties)
+    if o is None:
+        col = torch.arange(b, device="cuda").repeat_interleave(h.shape[1])
+    else:
+        col = torch.searchsorted(o, torch.arange(h.numel(), device="cuda", dtype=o.dtype),
+                                 right=True) - 1
+    h = h.reshape(-1)
+    valid = (h >= 0) & (h < n) & (col >= 0) & (col < b)
+    at, count = torch.unique(h[valid].long() * b + col[valid], return_counts=True)
+    p = {k: float(np.float32(v)) for k, v in {**dict(repeat=1, presence=0, frequency=0),
+                                               **penalties}.items()}
+    x = z.view(-1)[at].double()
+    x = torch.where(x > 0, x / p["repeat"], x * p["repeat"]) - p["presence"] - p["frequency"] * count
+    off = (got.view(-1)[at].double() - x).abs()
+    assert (off <= 2.0 ** -24 * x.abs() + 2.0 ** -150).all()
+    rest = got.clone()
+    rest.view(-1)[at] = z.view(-1)[at]
+    assert torch.equal(rest, z)
+
+
+def table(ids, slices):
+    """(place, slice) of ids in the table that counts a long column's."""
+    h = ids.astype(np.uint32) * np.uint32(0x9E3779B9)
+    h = (h ^ h >> np.uint32(15)) * np.uint32(0x9E3779B9)
+    return h % 2048, (h.astype(np.uint64) * np.uint64(slices) >> np.uint64(32)).astype(np.int64)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["one slice", "few places of one slice", "any"])
+def test_ids_that_a_table_cannot_hold(chain, kind):
+    """65,536 ids of one slice of a table with 2048 places, and 512 ids of 16 places."""
+    g = np.random.default_rng(5)
+    n = 1 << 24
+    ids = np.arange(n)
+    place, sl = table(ids, 256)  # the slice's upper 8 bits: one slice of up to 256, too
+    if kind != "any":
+        ids = ids[(sl == 37) & (place < (2048 if kind == "one slice" else 16))]
+        assert len(ids) > (50_000 if kind == "one slice" else 400)
+    for length in (9000, 140_000):
+        history = g.choice(ids, length)
+        history[::9] = history[0]
+        history[4::17] = -1
+        check(chain, n, 1, history[None], None, length, **PENALTIES)
+
+
+@pytest.mark.gpu
+def test_ids_that_only_places_of_their_own_hold(chain):
+    """Columns of two slices, 1500 ids of 512 places in one of them, among 16,384 rows:
+    an eighth of those is the table's size."""
+    g = np.random.default_rng(6)
+    n, b, length = 16_384, 520, 2000
+    place, sl = table(np.arange(n), 2)
+    ids = np.flatnonzero((sl == 1) & (place < 512))
+    assert len(ids) > 1500
+    history = g.choice(ids, (b, length))
+    history[1::3] = g.integers(-1, n, history[1::3].shape)
+    check(chain, n, b, history, None, 6, **PENALTIES)
+
+
+@pytest.mark.gpu
+def test_a_column_of_two_million_ids(chain):
+    """2,000,000 different ids, 1954 slices of the table."""
+    n = 2_000_003
+    check(chain, n, 1, np.random.default_rng(7).permutation(n)[None, :2_000_000], None, 7,
+          **PENALTIES)
