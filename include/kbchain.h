@@ -174,7 +174,8 @@ typedef struct {
 /* out [n][b], float, of logits z [n][b] of `type`; out must not overlap z.  Every
  * element is rounded to float once, n < 2^31 - 1.  KBC_EINVAL also where a penalty of
  * all columns is not finite or repeat_all not positive (a column's own repeat has to
- * be positive too; it is not checked). */
+ * be positive too; it is not checked).  With a frequency a column may have up to 2^26
+ * ids (with offsets: all of them together), else KBC_EINVAL. */
 kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, const kbc_limits *l,
                          float fill, float *out, void *stream);
 

@@ -457,7 +457,8 @@ def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0
     i % 32 of word i // 32 row i's: [ceil(n / 32)] or [ceil(n / 32)][b].  history: ids,
     one row a column of a 2-D tensor, or 1-D with offsets (b + 1 of them, not
     decreasing, of the ids' type); ids outside [0, n) are padding.  repeat (positive),
-    presence, frequency: numbers, or float32 [b], one a column.  A column that nothing
+    presence, frequency: numbers, or float32 [b], one a column; with a frequency a
+    history has up to 2**26 ids, or all ragged ones together.  A column that nothing
     is left to is `fill` throughout: chain.softmax makes NaN of it where fill is -inf,
     equal parts where it is finite; chain.softmax_xent wants a finite fill.
     Differentiable with respect to z and bias.

@@ -347,7 +347,7 @@ constexpr int kBlockIds = 2048;                      // ids in LDS at a time
 constexpr int kCompare = 4;                          // quads of them in flight
 
 template <class T, bool BACKWARD, int LANES>
-__global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) {
+__global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p, int64_t longest) {
   constexpr int kEntries = kThreads / LANES;  // of a workgroup
   __shared__ int4 lds[kBlockIds / 4];
   __shared__ int64_t range[2];
@@ -359,9 +359,12 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
   int id = -1;
   int64_t begin = t, end = t + 1;  // the ids of the entry's column
   if (col >= 0) {
-    id = row_of(p, a.n, t);
-    begin = bag_begin(p.columns, col);
-    end = bag_begin(p.columns, col + 1);
+    const int64_t b0 = bag_begin(p.columns, col), b1 = bag_begin(p.columns, col + 1);
+    if (b1 - b0 <= longest) {  // else table_kernel's
+      id = row_of(p, a.n, t);
+      begin = b0;
+      end = b1;
+    }
   }
   const bool valid = id >= 0;  // the same for the lanes of an entry
   const bool counts = !BACKWARD && (p.frequency || p.frequency_all != 0.0f);
@@ -423,6 +426,12 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
         ok ? penalised(p, (int32_t)col, z, count, bias_of(a, id, (int32_t)col)) : a.fill;
 }
 
+// Few columns are shared by workgroups that take a slice each, up to this many in all,
+// of 512 ids at least (8 columns of 1900 in slices of 1024 9.9 us, 512 9.7, 256 10.3; one of
+// 16000 22, 19 and 17, one of 100000 60, 52 and 55).
+constexpr int64_t kTableBlocks = 512;
+constexpr int64_t kShare = 512;
+
 // The forward pass where columns have many ids: a workgroup puts a column's ids
 // into a table in LDS and counts them there, a slice of the ids at a time (by hash,
 // at most about half as many as the table holds), then each place of the table writes
@@ -431,14 +440,20 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p) 
 // table holds them; at the latest a range has a place for each of its ids.
 // (1024 threads and 4096 places: 128 columns of 4000 ids 35 us for 29, 1024 of 64 30 for
 // 24, one of 16000 19 for 19.)
-template <class T>
-__global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties p, int parts) {
+//
+// Ragged columns differ: one may have nearly all of the ids.  Those of more than
+// `longest` ids are shared by the first `sharing` workgroups, kShare ids of the list to
+// each of them in turn; of the others each takes a part of one column.  (SHARING: there are
+// such; without, 20,000 columns of 64 ids take 120 us for 129.)
+template <class T, bool SHARING>
+__global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties p, int parts,
+                                                              int sharing, int64_t longest) {
   __shared__ int4 keys4[kTableThreads], counts4[kTableThreads];
   __shared__ int full;  // the last turn in which an id found no place
   int *keys = reinterpret_cast<int *>(keys4), *counts = reinterpret_cast<int *>(counts4);
-  const int32_t col = (int32_t)blockIdx.x / parts;
-  const int64_t begin = bag_begin(p.columns, col), end = bag_begin(p.columns, col + 1);
-  const int slices = end > begin ? max(parts, (int)((end - begin + kSlice - 1) / kSlice)) : 0;
+  int32_t col = 0;  // the column at hand, its ids and their slices
+  int64_t begin = 0, end = 0;
+  int slices = 0;
   // What an element is made of, and its place once its ids are counted.
   struct Element {
     float z, bias;
@@ -499,16 +514,58 @@ __global__ __launch_bounds__(kTableThreads) void table_kernel(Args a, Penalties 
       if (id[u] >= 0) write(id[u], count[u], e[u]);
     return true;
   };
-  for (int slice = (int)blockIdx.x % parts; slice < slices; slice += parts) {
-    // 2^bits ranges (at most 8 n / kTable, so the products fit).
-    for (int64_t r = 0, bits = 0; r >> bits == 0;) {
-      const int64_t lo = a.n * r >> bits, hi = a.n * (r + 1) >> bits;
-      if (count_range(slice, (int)lo, (uint32_t)(hi - lo))) {
-        ++r;
-      } else {  // what is left, in narrower ranges
-        bits += 3;
-        r <<= 3;
+  // Slices part, part + of, .. of the column at hand.
+  auto take = [&](int part, int of) {
+    slices = max(of, (int)((end - begin + kSlice - 1) / kSlice));
+    for (int slice = part; slice < slices; slice += of) {
+      // 2^bits ranges (at most 8 n / kTable, so the products fit).
+      for (int64_t r = 0, bits = 0; r >> bits == 0;) {
+        const int64_t lo = a.n * r >> bits, hi = a.n * (r + 1) >> bits;
+        if (count_range(slice, (int)lo, (uint32_t)(hi - lo))) {
+          ++r;
+        } else {  // what is left, in narrower ranges
+          bits += 3;
+          r <<= 3;
+        }
       }
+    }
+  };
+  const int own = (int)blockIdx.x - (SHARING ? sharing : 0);
+  if (own >= 0) {
+    col = own / parts;
+    begin = bag_begin(p.columns, col);
+    end = bag_begin(p.columns, col + 1);
+    if (end > begin && (!SHARING || end - begin <= longest)) take(own % parts, parts);
+    return;
+  }
+  if constexpr (SHARING) {
+    // A column of more than `longest` ids has one of every longest-th of the list; the
+    // first of them finds it.
+    __shared__ int32_t found[kTableThreads];
+    __shared__ unsigned long long any[kTableThreads / kWave];
+    const int64_t total = p.columns.tokens;
+    for (int64_t base = 0; base * longest < total; base += kTableThreads) {
+      const int64_t t = (base + threadIdx.x) * longest;
+      int64_t c = t < total ? bag_of(p.columns, t) : -1;
+      if (c >= 0) {
+        const int64_t b0 = bag_begin(p.columns, c), b1 = bag_begin(p.columns, c + 1);
+        if (b1 - b0 <= longest || t - longest >= b0) c = -1;
+      }
+      const unsigned long long mask = __ballot(c >= 0);
+      __syncthreads();  // the last ones have been read
+      found[threadIdx.x] = (int32_t)c;
+      if (threadIdx.x % kWave == 0) any[threadIdx.x / kWave] = mask;
+      __syncthreads();
+      for (int w = 0; w < kTableThreads / kWave; ++w)
+        for (unsigned long long m = any[w]; m; m &= m - 1) {  // uniform
+          col = found[w * kWave + __builtin_ctzll(m)];
+          begin = bag_begin(p.columns, col);
+          end = bag_begin(p.columns, col + 1);
+          const int shares = (int)min((int64_t)sharing, (end - begin + kShare - 1) / kShare);
+          const int first = (int)(begin / kShare % sharing);
+          const int mine = ((int)blockIdx.x - first + sharing) % sharing;
+          if (mine < shares) take(mine, shares);
+        }
     }
   }
 }
@@ -565,31 +622,44 @@ Penalties penalties_for(int32_t b, const kbc_limits *l) {
 // and 17, of 4000 196 and 29, 1024 of 64 29 and 24; but 93 of 32 9.7 and 9.8, 20000 of 64
 // 240 and 117, of 16 70 and 109.
 constexpr int64_t kLongColumn = 64;
-// Few columns are shared by workgroups that take a slice each, up to this many in all,
-// of 512 ids at least (8 columns of 1900 in slices of 1024 9.9 us, 512 9.7, 256 10.3; one of
-// 16000 22, 19 and 17, one of 100000 60, 52 and 55).
-constexpr int64_t kTableBlocks = 512;
-constexpr int64_t kShare = 512;
+// Ragged columns' lengths are on the device.  Lists of more ids than kSkewed, where
+// one column may hold them all, have their columns of more than kLongest ids shared by
+// up to kTableBlocks workgroups (20,000 columns, one of which has 1.2 million ids, 1.7 ms;
+// with the launch, and nothing to share, 20,000 of 16 85 us for 77, of 64 140 for 128).
+constexpr int64_t kSkewed = 16384;
+constexpr int64_t kLongest = 4096;
+// What is counted is read once for every kSlice ids of a column: 2^20 ids of one take
+// 0.9 ms, 2^22 13.5, so 2^26 seconds, and 2^30 would take a quarter of an hour.
+constexpr int64_t kMostCounted = int64_t(1) << 26;
+
+bool counts_ids(const kbc_limits *l) {
+  return l->entries > 0 && (l->frequency || l->frequency_all != 0.0f);
+}
 
 template <class T, bool BACKWARD>
 void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
   const int64_t total = h.columns.tokens;
   const bool counts = !BACKWARD && (h.frequency || h.frequency_all != 0.0f);
-  if constexpr (!BACKWARD)
-    if (counts && total / a.b >= kLongColumn && a.b <= kMostBlocks / 4) {
-      const int64_t parts = std::clamp<int64_t>(kTableBlocks / a.b, 1, ceil_div(total, kShare));
-      hipLaunchKernelGGL((table_kernel<T>), dim3((unsigned)(a.b * parts)), dim3(kTableThreads), 0,
-                         s, a, h, (int)parts);
-      return;
-    }
+  const bool skewed = counts && h.columns.offsets.p && total > kSkewed;
+  const int64_t longest = skewed ? kLongest : INT64_MAX;
+  const int sharing = skewed ? (int)std::min(kTableBlocks, ceil_div(total, kShare)) : 0;
+  const bool by_table = counts && total / a.b >= kLongColumn && a.b <= kMostBlocks / 4;
   auto go = [&](auto kernel, int lanes) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(total, kThreads / lanes)), dim3(kThreads), 0,
-                       s, a, h);
+                       s, a, h, longest);
   };
-  if (counts)
-    go(history_kernel<T, BACKWARD, kCountLanes>, kCountLanes);
-  else
+  if (!counts)
     go(history_kernel<T, BACKWARD, kFindLanes>, kFindLanes);
+  else if (!by_table)
+    go(history_kernel<T, BACKWARD, kCountLanes>, kCountLanes);
+  if constexpr (!BACKWARD)
+    if (by_table || skewed) {
+      const int64_t parts = std::clamp<int64_t>(kTableBlocks / a.b, 1, ceil_div(total, kShare));
+      const int64_t blocks = sharing + (by_table ? a.b * parts : 0);
+      const auto kernel = skewed ? table_kernel<T, true> : table_kernel<T, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kTableThreads), 0, s, a, h, (int)parts,
+                         sharing, longest);
+    }
 }
 
 // Few ids over a small array, which every workgroup then reads: at most 1024, and 2^28
@@ -653,6 +723,7 @@ extern "C" {
 kbc_status kbc_constrain(int64_t n, int32_t b, const void *z, kbc_type type, const kbc_limits *l,
                          float fill, float *out, void *stream) {
   if (bad_limits(n, b, type, l) || !z || !out) return KBC_EINVAL;
+  if (counts_ids(l) && (l->offsets ? l->entries : l->entries / b) > kMostCounted) return KBC_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Args a = args_for(n, b, l);
   a.z = z;

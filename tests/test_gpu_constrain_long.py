@@ -93,3 +93,61 @@ def test_a_column_of_two_million_ids(chain):
     n = 2_000_003
     check(chain, n, 1, np.random.default_rng(7).permutation(n)[None, :2_000_000], None, 7,
           **PENALTIES)
+
+
+def uneven(g, n, lengths):
+    """A history of columns of these lengths, a third of it padding or one id."""
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    history = g.integers(0, n, offsets[-1])
+    history[::5] = -1
+    history[1::7] = n // 2
+    return history, offsets
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at", [0, 9_999, 19_999])
+def test_one_column_of_nearly_all_ids(chain, at):
+    """20,000 columns of 60 ids on average, 1.2 million of them in one."""
+    g = np.random.default_rng(at)
+    lengths = g.integers(0, 2, 20_000)
+    lengths[at] = 1_200_000
+    check(chain, 300, 20_000, *uneven(g, 300, lengths), at, **PENALTIES)
+    lengths[at] = 150_000
+    lengths[(at + 20) % 20_000] = 90_001
+    check(chain, 300, 20_000, *uneven(g, 300, lengths), at, **PENALTIES)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lengths", [
+    [4096, 4097, 4095, 0, 1, 8192, 8193, 4096],      # at the length that is shared
+    [16_384], [16_385], [0, 0, 16_384, 0, 1],        # at the number from which any is
+    [5000] * 13 + [0] * 2000,                        # 31 a column
+    [5000] * 13 + [0] * 800,                         # 80 a column
+    [0, 300_000, 0, 0, 250_000, 1, 70_000] + [33] * 90,
+    [3] * 600 + [40_000] + [3] * 600])
+def test_uneven_columns(chain, lengths):
+    g = np.random.default_rng(len(lengths))
+    history, offsets = uneven(g, 5000, lengths)
+    check(chain, 5000, len(lengths), history, offsets, 8, **PENALTIES)
+    check(chain, 5000, len(lengths), history, offsets, 8, repeat=1.5)
+    # Ids before the first column and behind the last one are of none.
+    check(chain, 5000, len(lengths), np.concatenate([history, history])[:len(history) + 9000],
+          offsets + 5003, 8, **PENALTIES)
+
+
+def test_refused_lengths():
+    """More ids in one column than a frequency counts, before anything is enqueued."""
+    from paper_2002_06115_amd import chain as c
+    import ctypes
+    d = ctypes.c_void_p(256)  # never dereferenced
+
+    def forward(b, entries, offsets, **change):
+        l = c._Limits(repeat_all=1.0, id_bytes=8, entries=entries, history=256, offsets=offsets)
+        for k, v in change.items():
+            setattr(l, k, v)
+        return c._lib.kbc_constrain(10, b, d, 0, ctypes.byref(l), 0.0, d, None)
+
+    for change in (dict(frequency_all=0.5), dict(frequency=256)):
+        assert forward(2, (1 << 26) + 2, 256, **change) == 1
+        assert forward(2, (1 << 27) + 2, None, **change) == 1
+        assert forward(1, (1 << 26) + 1, None, **change) == 1
