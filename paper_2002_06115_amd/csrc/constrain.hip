@@ -73,7 +73,7 @@ struct Four {
   int m;
 };
 __device__ __forceinline__ bool one_row(const Args &a, const Four &p) {
-  return p.m == 4 && p.col + 4 <= a.b;
+  return p.m == 4 && p.col <= a.b - 4;  // (b may be 2^31 - 1)
 }
 // idx(row, column) of each of the four, the first's again where there are less.
 template <class F>

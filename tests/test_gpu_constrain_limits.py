@@ -1,0 +1,32 @@
+"""chain.constrain at the ends of its sizes."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def chain():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2002_06115_amd import chain
+    return chain
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mask", ["bool_row", "bits"])
+def test_columns_to_the_last(chain, mask):
+    """Two rows of 2^31 - 3 columns, the first masked: the four elements from the last of
+    the one row are of both."""
+    import torch
+    b = (1 << 31) - 3
+    z = torch.ones((2, b), dtype=torch.bfloat16, device="cuda")
+    if mask == "bool_row":
+        allowed = torch.tensor([False, True], device="cuda")
+    else:
+        allowed = torch.full((1, b), 2, dtype=torch.int32, device="cuda")
+    bias = torch.tensor([5.0, 0.5], device="cuda")
+    out = chain.constrain(z, bias=bias, allowed=allowed, fill=-2.0)
+    assert float(out[0].max()) == -2.0 == float(out[0].min())
+    assert float(out[1].max()) == 1.5 == float(out[1].min())
+    dz, _ = chain.constrain_backward(out, allowed=allowed, dtype=torch.bfloat16)
+    assert float(dz[0].max()) == 0.0 == float(dz[0].min())
+    assert float(dz[1].max()) == 1.5 == float(dz[1].min())
