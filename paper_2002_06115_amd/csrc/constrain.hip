@@ -347,13 +347,14 @@ constexpr int kBlockIds = 2048;                      // ids in LDS at a time
 constexpr int kCompare = 4;                          // quads of them in flight
 
 template <class T, bool BACKWARD, int LANES>
-__global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p, int64_t longest) {
-  constexpr int kEntries = kThreads / LANES;  // of a workgroup
+__global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p, int64_t from,
+                                                           int64_t longest) {
+  constexpr int kEntries = kThreads / LANES;  // of a workgroup, those of the launch from `from` on
   __shared__ int4 lds[kBlockIds / 4];
   __shared__ int64_t range[2];
   int *ids = reinterpret_cast<int *>(lds);
   const int lane = threadIdx.x % LANES;
-  const int64_t t0 = (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / LANES;
+  const int64_t t0 = from + (int64_t)blockIdx.x * kEntries, t = t0 + threadIdx.x / LANES;
   const int64_t total = p.columns.tokens;
   const int64_t col = t < total ? bag_of_lanes<LANES>(p.columns, t, lane) : -1;
   int id = -1;
@@ -644,9 +645,11 @@ void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
   const int64_t longest = skewed ? kLongest : INT64_MAX;
   const int sharing = skewed ? (int)std::min(kTableBlocks, ceil_div(total, kShare)) : 0;
   const bool by_table = counts && total / a.b >= kLongColumn && a.b <= kMostBlocks / 4;
-  auto go = [&](auto kernel, int lanes) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(total, kThreads / lanes)), dim3(kThreads), 0,
-                       s, a, h, longest);
+  auto go = [&](auto kernel, int lanes) {  // as many ids at a time as a grid holds
+    const int64_t per_block = kThreads / lanes, most = kMostBlocks * per_block;
+    for (int64_t from = 0; from < total; from += most)
+      hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(std::min(most, total - from), per_block)),
+                         dim3(kThreads), 0, s, a, h, from, longest);
   };
   if (!counts)
     go(history_kernel<T, BACKWARD, kFindLanes>, kFindLanes);

@@ -30,3 +30,23 @@ def test_columns_to_the_last(chain, mask):
     dz, _ = chain.constrain_backward(out, allowed=allowed, dtype=torch.bfloat16)
     assert float(dz[0].max()) == 0.0 == float(dz[0].min())
     assert float(dz[1].max()) == 1.5 == float(dz[1].min())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("columns,length,frequency", [(1 << 23, 33, 0.25), (1 << 24, 64, 0.0)])
+def test_ids_past_one_grid(chain, columns, length, frequency):
+    """277 million ids that are counted, and the 2^30 that a call takes at most: ids of a
+    row that only the last columns have had."""
+    import torch
+    history = torch.full((columns, length), -1, dtype=torch.int32, device="cuda")
+    history[-7:, -1] = 1
+    history[-5:, 0] = 1
+    z = torch.ones((2, columns), device="cuda")
+    out = chain.constrain(z, history=history, presence=0.5, frequency=frequency)
+    assert (out[0] == 1.0).all() and (out[1, :-7] == 1.0).all()
+    want = [0.5 - frequency] * 2 + [0.5 - 2 * frequency] * 5
+    assert out[1, -7:].tolist() == want
+    if not frequency:
+        dz, _ = chain.constrain_backward(out, z, None, history, repeat=4.0)
+        assert torch.equal(dz[0], out[0]) and torch.equal(dz[1, :-7], out[1, :-7])
+        assert (dz[1, -7:] == 0.125).all()
