@@ -956,15 +956,19 @@ kbc_status kbc_embed(int64_t tokens, const void *ids, int32_t id_bytes, int64_t 
     return KBC_EINVAL;
   if (tokens == 0) return KBC_OK;
   if (!ids || !out) return KBC_EINVAL;
-  const int per_block = kThreads / group_lanes(type, dim) * kLookupRows;
-  if (ceil_div(tokens, per_block) > kMostBlocks) return KBC_EINVAL;
-  const LookupArgs a{{ids, id_bytes}, tokens, rows, dim, table, stride, scale, out};
   hipStream_t s = static_cast<hipStream_t>(stream);
   with_rows(type, dim, [&](auto t, auto vec, auto lanes) {
     using T = decltype(t);
     constexpr int V = decltype(vec)::value, L = decltype(lanes)::value;
-    const dim3 grid((unsigned)ceil_div(tokens, kThreads / L * kLookupRows));
-    hipLaunchKernelGGL((lookup_kernel<T, V, L>), grid, dim3(kThreads), 0, s, a);
+    constexpr int64_t kPerBlock = kThreads / L * kLookupRows;
+    // As many tokens at a time as a grid holds.
+    for (int64_t from = 0; from < tokens; from += kMostBlocks * kPerBlock) {
+      const int64_t n = std::min(kMostBlocks * kPerBlock, tokens - from);
+      const LookupArgs a{{static_cast<const char *>(ids) + from * id_bytes, id_bytes},
+                         n, rows, dim, table, stride, scale, static_cast<T *>(out) + from * dim};
+      hipLaunchKernelGGL((lookup_kernel<T, V, L>), dim3((unsigned)ceil_div(n, kPerBlock)),
+                         dim3(kThreads), 0, s, a);
+    }
   });
   return launched();
 }
