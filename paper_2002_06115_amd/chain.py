@@ -211,6 +211,14 @@ def _run(fn, what, device, *args):
     _ok(status, what)
 
 
+def _differentiated(*tensors):
+    """Whether autograd has to see a call of these: one of them asks for a gradient, or
+    carries a tangent (forward mode, which the functions refuse)."""
+    return any(isinstance(t, torch.Tensor) and
+               (t.requires_grad and torch.is_grad_enabled() or
+                torch.autograd.forward_ad.unpack_dual(t).tangent is not None) for t in tensors)
+
+
 def _bytes(n, device):
     """(tensor, address, bytes) of n bytes of scratch; the tensor is held until
     the call is enqueued."""
@@ -325,9 +333,10 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     ids[offsets[g]:offsets[g + 1]] of a 1-D ids.  An id outside [0, rows) stands for
     padding: zeros, no term, not counted by the mean, no gradient; a bag of nothing
     else is zeros.  ids and offsets are contiguous int32 or int64; a row of table is
-    adjacent values, rows may lie apart.  Differentiable with respect to table.
+    adjacent values, rows may lie apart.  Differentiable (backwards) with respect to
+    table.
     """
-    if isinstance(table, torch.Tensor) and table.requires_grad and torch.is_grad_enabled():
+    if _differentiated(table):
         return _Embed.apply(table, ids, offsets, scale, pool)
     return _embed_forward(table, ids, offsets, scale, pool)[0]
 
@@ -461,11 +470,10 @@ def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0
     history has up to 2**26 ids, or all ragged ones together.  A column that nothing
     is left to is `fill` throughout: chain.softmax makes NaN of it where fill is -inf,
     equal parts where it is finite; chain.softmax_xent wants a finite fill.
-    Differentiable with respect to z and bias.
+    Differentiable (backwards) with respect to z and bias.
     """
     args = (z, bias, allowed, history, offsets, repeat, presence, frequency, fill)
-    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
-                                       for t in (z, bias)):
+    if _differentiated(z, bias):
         return _Constrain.apply(*args)
     return _constrain_forward(*args)[0]
 
