@@ -498,10 +498,13 @@ _FollowFns = None
 
 
 def _follow_fn(pack):
+    import torch
     global _FollowFns
     if _FollowFns is None:
         _FollowFns = _make_functions()
-    return _FollowFns[1 if pack else 0]
+    # Without a backward pass to come nothing is kept.  (The functions' own
+    # needs_input_grad does not tell: it is that of the inputs, whatever the mode.)
+    return _FollowFns[1 if pack and torch.is_grad_enabled() else 0]
 
 
 def follow(kb: KB, X, R, pack: bool = False):

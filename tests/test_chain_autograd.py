@@ -45,3 +45,41 @@ def test_no_graph_without_a_gradient(plain):
         assert not chain.constrain(z, bias=bias).requires_grad
     with torch.inference_mode():
         assert not chain.embed(table, ids).requires_grad
+
+
+class _Hop:
+    """A KB's two calls in torch: Y = X * R's sum, elementwise enough for a graph."""
+    def follow(self, X, R, residual=None):
+        return X.detach() * R.detach().sum(0)
+
+    def follow_backward(self, X, R, dY, want_dx=True, want_dr=True, residual=None):
+        return (dY * 2.0 if want_dx else None), (X if want_dr else None)
+
+
+def test_sets_are_packed_only_for_a_backward_pass(monkeypatch):
+    import types
+    import paper_2002_06115_amd as kbf
+    packed = []
+
+    def pack(X):
+        packed.append(X)
+        return types.SimpleNamespace(data=X.detach().clone())
+
+    monkeypatch.setattr(kbf, "_packed", pack)
+    monkeypatch.setattr(kbf, "Packed", lambda data, b: data)
+    X, R = torch.ones(2, 3), torch.ones(2, 3)
+    for leaf in (X.clone().requires_grad_(), X):
+        R_leaf = R.clone().requires_grad_()
+        for mode in (torch.no_grad, torch.inference_mode):
+            with mode():
+                for follow in (kbf.follow, kbf.follow_residual):
+                    assert torch.equal(follow(_Hop(), leaf, R_leaf, pack=True), 2 * X)
+        assert not packed
+        Y = kbf.follow(_Hop(), leaf, R_leaf, pack=True)
+        assert len(packed) == 1
+        Y.sum().backward()
+        assert torch.equal(R_leaf.grad, X)
+        packed.clear()
+    leaf = X.clone().requires_grad_()
+    kbf.follow(_Hop(), leaf, R, pack=True).sum().backward()  # dX needs no set
+    assert not packed and torch.equal(leaf.grad, 2 * X)
