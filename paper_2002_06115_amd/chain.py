@@ -362,14 +362,6 @@ def _limits(n, b, device, bias, allowed, history, offsets, penalties):
         if tuple(allowed.shape) not in ((rows,), (rows, b)) or not allowed.is_contiguous():
             raise ValueError(f"allowed must be contiguous, of shape {(rows,)} or {(rows, b)}")
         l.allowed, l.allowed_each = allowed.data_ptr(), allowed.dim() == 2
-    if history is None:
-        if offsets is not None:
-            raise ValueError("offsets go with a history")
-        return l
-    columns, l.offsets = _bag_args(history, offsets, "sum", device)
-    if columns != b:
-        raise ValueError(f"history must be of {b} columns")
-    l.history, l.entries, l.id_bytes = history.data_ptr(), history.numel(), history.element_size()
     for name, value in penalties.items():
         if isinstance(value, torch.Tensor):
             if value.dtype != torch.float32 or value.device != device:
@@ -382,6 +374,14 @@ def _limits(n, b, device, bias, allowed, history, offsets, penalties):
             if not -3.0e38 < value < 3.0e38 or (name == "repeat" and value <= 0.0):
                 raise ValueError(f"{name} must be finite, and repeat positive")
             setattr(l, name + "_all", value)
+    if history is None:
+        if offsets is not None:
+            raise ValueError("offsets go with a history")
+        return l
+    columns, l.offsets = _bag_args(history, offsets, "sum", device)
+    if columns != b:
+        raise ValueError(f"history must be of {b} columns")
+    l.history, l.entries, l.id_bytes = history.data_ptr(), history.numel(), history.element_size()
     return l
 
 
