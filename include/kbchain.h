@@ -106,7 +106,7 @@ kbc_status kbc_softmax_xent_scratch(int64_t n, int32_t b, const float *z, const 
  *   out, dout, dtable : contiguous, of `type`.
  * Any element alignment will do.  1 <= rows < 2^31 - 1, tokens <= 2^30, bags <
  * 2^31 - 1 (2^25 with mean), 1 <= dim <= 65536, else KBC_EINVAL.  Sums are taken in double, in a
- * fixed order (partial sums of 16-bit outputs in float); an output is rounded to
+ * fixed order (partial sums of float16 outputs in float); an output is rounded to
  * float, and to a 16-bit type from there.
  */
 typedef enum { KBC_F32 = 0, KBC_BF16 = 1, KBC_F16 = 2 } kbc_type;

@@ -587,11 +587,13 @@ struct SumArgs {
   void *slots;  // Slot<type> [chunk][2][dim]: the sum of the chunk's first row, if it began
                 // before the chunk, and of its last one, if it began in it and goes on
 };
-// Partial sums of a row: double, and float where the row is rounded to 16 bits in the
-// end, 2^-24 of them against its 2^-9 or 2^-12 (half the bytes, a tenth of all that
-// the sum over 262144 tokens of 512 float16 values moves).
+// Partial sums of a row: double, and float where the row is rounded to float16 in the
+// end, 2^-24 of them against its 2^-12 (half the bytes, a tenth of all that the sum over
+// 262144 tokens of 512 values moves).  Sums of 2^30 float16 values are far from a float's
+// end, but those of a few bfloat16 values may pass it, where the scale or the mean, or
+// other terms, bring the row back.
 template <class T>
-using Slot = std::conditional_t<sizeof(T) == 2, float, double>;
+using Slot = std::conditional_t<std::is_same_v<T, _Float16>, float, double>;
 
 constexpr int kSumRows = 8;  // of a lane group in flight
 
@@ -871,7 +873,7 @@ Scratch scratch_for(int64_t tokens, int64_t bags, int32_t dim, bool sorted, bool
     s.weights = take(bags * 8);
   }
   const int64_t chunks = ceil_div(tokens, chunk_for(tokens, lpg));
-  if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);  // (half of it with 16-bit types)
+  if (chunks > 1) s.slots = take(chunks * 2 * dim * 8);  // (half of it with float16)
   s.bytes = at;
   return s;
 }

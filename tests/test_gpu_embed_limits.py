@@ -31,3 +31,34 @@ def test_tokens_past_one_grid(chain):
         assert torch.equal(part[:, 0], want[:, 0]) and torch.equal(part[:, -1], want[:, -1])
     del out, ids
     torch.cuda.empty_cache()  # for the tests after this one
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [3, 64, 1001])
+@pytest.mark.parametrize("tokens", [700, 5000, 70_000])
+def test_large_values(chain, tokens, dim):
+    """Sums that pass a float's range on the way to a mean, or to a scaled sum, that does
+    not: powers of two, so every step is exact."""
+    import torch
+    top = 2.0 ** 127
+    table = torch.full((3, dim), top, dtype=torch.bfloat16, device="cuda")
+    table[1] = -top
+    ids = torch.zeros(tokens, dtype=torch.int64, device="cuda")
+    offsets = torch.tensor([0, tokens], device="cuda")
+    mean = chain.embed(table, ids, offsets, pool="mean")
+    assert (mean == top).all()
+    n = tokens // 64 * 64
+    small = chain.embed(table, ids[:n], offsets.clamp(max=n), scale=2.0 ** -20, pool="sum")
+    assert (small == torch.tensor(n * 2.0 ** 107).to(torch.bfloat16).item()).all()
+    ids[tokens // 2:tokens // 2 * 2] = 1  # as many of the opposite
+    ids[tokens // 2 * 2:] = -1
+    ids[0] = 2
+    table[2] = top / 2
+    total = chain.embed(table, ids, offsets, pool="sum")
+    assert (total == -top / 2).all()
+
+    dout = torch.full((tokens, dim), top, dtype=torch.bfloat16, device="cuda")
+    ids = torch.zeros(tokens, dtype=torch.int64, device="cuda")
+    back = chain.embed_backward(dout[:n], ids[:n], 2, scale=2.0 ** -20)
+    assert (back[0] == torch.tensor(n * 2.0 ** 107).to(torch.bfloat16).item()).all()
+    assert not back[1].any()
