@@ -183,7 +183,7 @@ class Packed:
         import torch
         if not isinstance(data, torch.Tensor) or data.dtype != torch.uint8 or not data.is_cuda:
             raise TypeError("data must be a uint8 CUDA tensor")
-        if b < 1 or data.dim() != 2 or data.shape[1] != _lib.kb_packed_pitch(int(b)) or \
+        if not 0 < b < 2 ** 31 or data.dim() != 2 or data.shape[1] != _lib.kb_packed_pitch(int(b)) or \
                 not data.is_contiguous():
             raise ValueError(f"data must be contiguous packed rows of {b} values")
         self.data, self.b = data, int(b)
@@ -216,6 +216,8 @@ def pack(X):
         raise TypeError("X must be a float32 CUDA tensor")
     if X.dim() != 2 or X.shape[1] < 1 or not X.is_contiguous():
         raise ValueError("X must be a contiguous [rows][b] tensor")
+    if X.shape[1] >= 2 ** 31:  # the C argument has 32 bits; ctypes would cut the others off
+        raise ValueError("X must have less than 2^31 columns")
     return _packed(X)
 
 

@@ -75,12 +75,17 @@ for _f in (_softmax, _softmax_backward, _l1_normalize, _l1_normalize_backward, _
     _f.restype = ctypes.c_int
 
 
+_WIDEST = 2 ** 31 - 1  # the C arguments for widths are 32-bit; ctypes would cut more off
+
+
 def _mat(t, name, shape=None):
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_cuda:
         raise TypeError(f"{name} must be a float32 CUDA tensor")
     if t.dim() != 2 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [n][b] tensor")
+    if t.shape[1] > _WIDEST:
+        raise ValueError(f"{name} must have less than 2^31 columns")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}")
     return t
@@ -259,6 +264,8 @@ def _embed_forward(table, ids, offsets, scale, pool):
     if table.dim() != 2 or not table.numel():
         raise ValueError("table must be [rows][dim], not empty")
     rows, dim = table.shape
+    if dim > _WIDEST:
+        raise ValueError("a row of table must have less than 2^31 values")
     stride, step = table.stride()
     if (dim > 1 and step != 1) or (rows > 1 and stride < dim):
         raise ValueError("the values of a row of table must be adjacent, its rows apart")
@@ -303,8 +310,8 @@ def embed_backward(dout, ids, rows, offsets=None, scale=1.0, pool=None):
         raise ValueError("rows must be positive")
     bags, _ = _bag_args(ids, offsets, pool, dout.device)
     lead = tuple(ids.shape) if bags is None else (bags,)
-    if dout.dim() != len(lead) + 1 or tuple(dout.shape[:-1]) != lead or dout.shape[-1] < 1 or \
-            not dout.is_contiguous():
+    if dout.dim() != len(lead) + 1 or tuple(dout.shape[:-1]) != lead or \
+            not 0 < dout.shape[-1] <= _WIDEST or not dout.is_contiguous():
         raise ValueError(f"dout must be contiguous, of shape {lead} and a row's width")
     return _embed_gradient(dout, ids, offsets, rows, bags, float(scale), pool == "mean", code)
 
@@ -390,6 +397,8 @@ def _logits(z, name):
     code = _type(z, name)
     if z.dim() != 2 or z.shape[0] < 1 or z.shape[1] < 1 or not z.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [n][b] tensor, not empty")
+    if z.shape[1] > _WIDEST:
+        raise ValueError(f"{name} must have less than 2^31 columns")
     return z.shape[0], z.shape[1], code
 
 

@@ -39,3 +39,28 @@ def test_penalties_are_checked_without_a_history_on_the_gpu():
     assert torch.equal(zg.grad, z)
     with pytest.raises(ValueError):
         chain.constrain_backward(z, repeat=0.0)
+
+
+class OnTheGpu(torch.Tensor):
+    """A tensor without memory that says it is on a GPU."""
+    is_cuda = True
+
+
+def without_memory(*shape, dtype=torch.float32):
+    return torch.empty(shape, dtype=dtype, device="meta").as_subclass(OnTheGpu)
+
+
+def test_widths_past_32_bits():
+    """2^32 + 8 columns are not 8."""
+    import paper_2002_06115_amd as kbf
+    wide = without_memory(1, 2 ** 32 + 8)
+    ids = without_memory(1, dtype=torch.int64)
+    codes = without_memory(1, kbf._lib.kb_packed_pitch(8), dtype=torch.uint8)
+    for call in (lambda: chain.constrain(wide), lambda: chain.constrain_backward(wide),
+                 lambda: chain.constrain_backward(without_memory(1, 8), wide),
+                 lambda: chain.softmax(wide), lambda: chain.embed(wide, ids),
+                 lambda: chain.embed_backward(wide, ids, 1), lambda: kbf.pack(wide),
+                 lambda: kbf.Packed(codes, 2 ** 32 + 8)):
+        with pytest.raises(ValueError):
+            call()
+    assert kbf.Packed(codes, 8).b == 8
