@@ -216,8 +216,6 @@ def pack(X):
         raise TypeError("X must be a float32 CUDA tensor")
     if X.dim() != 2 or X.shape[1] < 1 or not X.is_contiguous():
         raise ValueError("X must be a contiguous [rows][b] tensor")
-    if X.shape[1] >= 2 ** 31:  # the C argument has 32 bits; ctypes would cut the others off
-        raise ValueError("X must have less than 2^31 columns")
     return _packed(X)
 
 
@@ -225,6 +223,8 @@ def _packed(X):
     """pack(X) of an X that has been checked."""
     import torch
     rows, b = X.shape
+    if b >= 2 ** 31:  # the C argument has 32 bits; ctypes would cut the others off
+        raise ValueError("X must have less than 2^31 columns")
     data = torch.empty((rows, _lib.kb_packed_pitch(b)), dtype=torch.uint8, device=X.device)
     _on_device(_lib.kb_pack, "kb_pack", X.device, rows, b, X.data_ptr(), data.data_ptr())
     return Packed(data, b)

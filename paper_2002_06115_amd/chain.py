@@ -19,6 +19,7 @@ import functools
 import os
 
 import torch
+from torch.autograd import forward_ad as _forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("KBCHAIN_LIB", os.path.join(_HERE, "_lib", "libkbchain.so"))
@@ -84,7 +85,7 @@ def _mat(t, name, shape=None):
         raise TypeError(f"{name} must be a float32 CUDA tensor")
     if t.dim() != 2 or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [n][b] tensor")
-    if t.shape[1] > _WIDEST:
+    if t.size(1) > _WIDEST:
         raise ValueError(f"{name} must have less than 2^31 columns")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}")
@@ -216,12 +217,9 @@ def _run(fn, what, device, *args):
     _ok(status, what)
 
 
-def _differentiated(*tensors):
-    """Whether autograd has to see a call of these: one of them asks for a gradient, or
-    carries a tangent (forward mode, which the functions refuse)."""
-    return any(isinstance(t, torch.Tensor) and
-               (t.requires_grad and torch.is_grad_enabled() or
-                torch.autograd.forward_ad.unpack_dual(t).tangent is not None) for t in tensors)
+def _asks(t):
+    """Whether t asks for a gradient."""
+    return isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled()
 
 
 def _bytes(n, device):
@@ -343,7 +341,8 @@ def embed(table, ids, offsets=None, scale=1.0, pool=None):
     adjacent values, rows may lie apart.  Differentiable (backwards) with respect to
     table.
     """
-    if _differentiated(table):
+    # (A tensor with a forward-mode tangent need not ask; the function refuses it.)
+    if _asks(table) or _forward_ad._current_level >= 0:
         return _Embed.apply(table, ids, offsets, scale, pool)
     return _embed_forward(table, ids, offsets, scale, pool)[0]
 
@@ -395,11 +394,12 @@ def _limits(n, b, device, bias, allowed, history, offsets, penalties):
 def _logits(z, name):
     """(rows, columns, type code) of logits."""
     code = _type(z, name)
-    if z.dim() != 2 or z.shape[0] < 1 or z.shape[1] < 1 or not z.is_contiguous():
+    n, b = z.shape if z.dim() == 2 else (0, 0)
+    if n < 1 or b < 1 or not z.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [n][b] tensor, not empty")
-    if z.shape[1] > _WIDEST:
+    if b > _WIDEST:
         raise ValueError(f"{name} must have less than 2^31 columns")
-    return z.shape[0], z.shape[1], code
+    return n, b, code
 
 
 def _constrain_forward(z, bias, allowed, history, offsets, repeat, presence, frequency, fill):
@@ -482,7 +482,7 @@ def constrain(z, bias=None, allowed=None, history=None, offsets=None, repeat=1.0
     Differentiable (backwards) with respect to z and bias.
     """
     args = (z, bias, allowed, history, offsets, repeat, presence, frequency, fill)
-    if _differentiated(z, bias):
+    if _asks(z) or _asks(bias) or _forward_ad._current_level >= 0:
         return _Constrain.apply(*args)
     return _constrain_forward(*args)[0]
 
