@@ -339,8 +339,11 @@ __global__ __launch_bounds__(kThreads) void row_kernel(Args a, Penalties h) {
 
 // Lanes that share an entry's count: 15200 ids of 8 columns take 14 us with 16 lanes,
 // 17 with 8, 27 with 4.  Where nothing is counted they only find the entry's column: 16
-// / 8 / 4 / 1 lanes take, with the dense launch, 8.3 / 8.6 / 8.5 / 9.5 us for 93 columns of
-// 3 ids, 55.6 / 38.3 / 28.7 / 25.7 for 128 of 4000, 49 / 35 / 30 / 22 for 20000 of 16.
+// / 8 lanes take, with the dense launch, 8.3 / 8.6 us for 93 columns of 3 ids, 56 / 38 for
+// 128 of 4000, 49 / 35 for 20000 of 16.  4 lanes against 1: 7.6 and 8.7 us for 93 columns
+// of 3 ids, 6.2 and 7.5 for 500 of 16, 5.5 and 6.0 for 8 of 2000, but from about 100,000 ids
+// on 1 lane is ahead, 9.4 and 8.7 for 128 of 1000, 27 and 22 for 128 of 4000, 36 and 30 for
+// 20000 of 16 (gradient 38.5 and 34.6): the histories of a model's columns are the shorter.
 constexpr int kCountLanes = 16;
 constexpr int kFindLanes = 4;
 constexpr int kBlockIds = 2048;                      // ids in LDS at a time
@@ -427,9 +430,11 @@ __global__ __launch_bounds__(kThreads) void history_kernel(Args a, Penalties p, 
         ok ? penalised(p, (int32_t)col, z, count, bias_of(a, id, (int32_t)col)) : a.fill;
 }
 
-// Few columns are shared by workgroups that take a slice each, up to this many in all,
-// of 512 ids at least (8 columns of 1900 in slices of 1024 9.9 us, 512 9.7, 256 10.3; one of
-// 16000 22, 19 and 17, one of 100000 60, 52 and 55).
+// Few columns are shared by workgroups that take a slice each: up to this many
+// workgroups, and a column up to one for every 512 ids of all columns together, not of its
+// own, as it may hold most of them.  (8 columns of 1900 ids, by the 256 / 512 / 1024 ids of
+// all columns 9.0 / 8.3 / 8.6 us, by 512 of its own 9.4; the same of uneven lengths 11.4 / 11.1
+// / 11.5 and 23; one column of 16000 16.1 / 17.9 / 24.4, of 100000 51 / 51 / 63.)
 constexpr int64_t kTableBlocks = 512;
 constexpr int64_t kShare = 512;
 
@@ -667,8 +672,11 @@ void launch_history(const Args &a, const Penalties &h, hipStream_t s) {
 
 // Few ids over a small array, which every workgroup then reads: at most 1024, and 2^28
 // for ids times elements.  One launch against two, forward us: 256 ids over 18 x 128
-// 5.8 and 8.0, 700 over 32000 x 1 6.2 and 8.7, 279 over 8000 x 93 6.4 and 8.7; 1000 over
-// 1000 x 1000 9.4 and 9.1, 279 over 43000 x 93 11.7 and 10.5 (not taken).
+// 3.5 and 5.7, 700 over 32000 x 1 4.0 and 7.4, 279 over 8000 x 93 3.9 and 6.1, 4 over a
+// million x 4 6.7 and 7.6; 1000 over 1000 x 1000 9.4 and 9.1, 279 over 43000 x 93 11.7 and
+// 10.5 (not taken).  Taken, and a loss, are up to 64 ids over more elements than kSmall: one
+// vector a thread costs more there than a launch, 4 ids over 16 million x 4 83 and 76, 8
+// over 4 million x 8 44 and 41, the gradients alike.
 bool few_ids(const Args &a, const kbc_limits *l) {
   return l->entries <= 1024 && a.b <= kFewColumns &&
          a.n * a.b <= (int64_t(1) << 28) / l->entries;

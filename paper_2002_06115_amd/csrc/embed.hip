@@ -839,9 +839,14 @@ void with_rows(kbc_type type, int32_t dim, F f) {
 }
 
 // Entries of a lane group: about 2048 waves' worth of groups over the list, at least
-// kSumRows entries each (gradient of 16389 tokens of 1001 bfloat16 values and of
-// 262144 of 512 float16: with 2048 waves 71 and 112 us, with 4096 77 and 112, with
-// 8192, and so more partial sums, 77 and 127).
+// kSumRows entries each.  More waves leave more partial sums, fewer leave CUs idle.
+// The gradient, with 1024 / 2048 / 4096 / 8192 waves, us:
+//   bfloat16  16,389 tokens of 1001 values   70 / 66 / 66 / 67
+//   float16   262,144 of 512                102 / 102 / 103 / 111
+//   float32   262,144 of 128, of 512         68 / 62 / 62 / 66, 141 / 141 / 147 / 154
+//   float32   30,000 of 300                  42 / 41 / 45 / 45
+//   float32   a million of 3                 76 / 76 / 79 / 82
+// and 100,000 of 8 or 64, 30,000 of 64 the same with all.
 int32_t run_for(int64_t tokens, int lpg) {
   int32_t run = kSumRows;
   while (run < 128 && tokens * lpg > (int64_t)run * 2048 * kWave) run *= 2;
