@@ -513,7 +513,8 @@ def follow(kb: KB, X, R, pack: bool = False):
     """Differentiable follow(X, R) (Eq. 4) on entity-major tensors X [N_E][b], R [N_R][b].
 
     With ``pack`` X is kept in 8 bits for the backward pass (see pack()):
-    R's gradient is that of the values kept, X's is the same."""
+    R's gradient is that of the values kept, X's is the same.  It saves memory where
+    nothing else keeps X in float (chain.l1_normalize's backward pass keeps its output)."""
     return _follow_fn(pack).apply(X, R, kb, None)
 
 
