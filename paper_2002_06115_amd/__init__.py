@@ -183,8 +183,8 @@ class Packed:
         import torch
         if not isinstance(data, torch.Tensor) or data.dtype != torch.uint8 or not data.is_cuda:
             raise TypeError("data must be a uint8 CUDA tensor")
-        if not 0 < b < 2 ** 31 or data.dim() != 2 or data.shape[1] != _lib.kb_packed_pitch(int(b)) or \
-                not data.is_contiguous():
+        if not 0 < b < 2 ** 31 or data.dim() != 2 or not data.is_contiguous() or \
+                data.shape[1] != _lib.kb_packed_pitch(int(b)):
             raise ValueError(f"data must be contiguous packed rows of {b} values")
         self.data, self.b = data, int(b)
 

@@ -151,3 +151,36 @@ def test_refused_lengths():
         assert forward(2, (1 << 26) + 2, 256, **change) == 1
         assert forward(2, (1 << 27) + 2, None, **change) == 1
         assert forward(1, (1 << 26) + 1, None, **change) == 1
+
+
+@pytest.mark.gpu
+def test_uneven_columns_replayed(chain):
+    """A captured call whose columns' lengths change between replays."""
+    import torch
+    g = np.random.default_rng(9)
+    n, b, total = 3000, 700, 40_000
+    z = torch.from_numpy(g.standard_normal((n, b)).astype(np.float32)).cuda()
+    h = torch.from_numpy(g.integers(-1, n, total)).cuda()
+    lengths = np.zeros((3, b), np.int64)
+    lengths[0, 5] = total
+    lengths[1] = total // b
+    lengths[2, [0, 350, 699]] = 20_000, 15_000, 5000
+    offsets = [torch.from_numpy(np.concatenate([[0], np.cumsum(l)])).cuda() for l in lengths]
+    o = offsets[0].clone()
+    call = lambda: chain.constrain(z, history=h, offsets=o, **PENALTIES)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    for k in (1, 2, 0, 1):
+        o.copy_(offsets[k])
+        h.copy_(h.roll(777))
+        graph.replay()
+        want = call()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), k
+    check(chain, n, b, h.cpu().numpy(), offsets[2].cpu().numpy(), 9, **PENALTIES)
